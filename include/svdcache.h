@@ -60,6 +60,7 @@ extern "C" {
 
 #define SVDCACHE_F32   0
 #define SVDCACHE_BF16  1
+#define SVDCACHE_FP8   2   /* 8-bit matrices (below): only where a call says so */
 
 /* Predictors of the principal coefficients on cached steps (Sec. 3.4; Sec. 5.3, Fig. 4(b)). */
 #define SVDCACHE_PREDICT_EMA     0  /* the method's own: the EMA state of Eq. 11                          */
@@ -321,6 +322,53 @@ SVDCACHE_API int svdcache_full_step_residual_ema_batched(int nblocks, const void
 SVDCACHE_API int svdcache_singular_values(const double *lambda, int k, double *sigma, void *stream);
 SVDCACHE_API int svdcache_left_factors(const float *C, const double *sigma, int64_t N, int k, float *U,
                           void *stream);
+
+/* ---------------------------------------------------------------------------------
+ * The 8-bit linear path around a cached block (no counterpart in the paper's equations; its
+ * Table 3 pairs the method with an 8-bit quantised model).  A full step needs the block's
+ * feature F from the network's own linear layers, and a cached step's Fhat is added to the
+ * residual stream before the next block's norm: these calls are those two neighbours.
+ *
+ * 8-bit matrix: rows of e4m3 values (one byte each, pitch ld in bytes) and a scale buffer.
+ *   - Every 1 x 128 group of a row has one scale, a power of two 2^e held as the byte e + 127
+ *     (E8M0).  e is the smallest integer with 448 * 2^e >= the group's largest finite magnitude
+ *     (0 for a group of zeros; e >= -127).  value = e4m3(y / 2^e), round to nearest even.
+ *   - Inf and NaN become the NaN code and stay with their element; the group's scale is that of
+ *     its finite elements.
+ *   - The scale buffer has svdcache_fp8_scale_bytes(rows, cols) bytes: pieces of 512 bytes for
+ *     128 rows x 4 groups, [rows / 128][groups / 4] rounded up; the byte of row m, group g is
+ *     byte (m % 32) * 16 + (m / 32 % 4) * 4 + g % 4 of piece (m / 128, g / 4).  Bytes of rows and
+ *     groups that do not exist are never written and reach no result.
+ *   - Limits: 0 <= rows < 2^31 - 256 (0 rows: nothing is launched), 1 <= cols <= 131072, values and
+ *     scales 16-byte aligned, pitch a multiple of 16 bytes.  cols itself need not be.
+ *
+ *   svdcache_quantize_fp8   X (rows x cols of F32 or BF16, pitch ld) -> Q, S.  tile_rows 1: a scale
+ *              per 1 x 128 group (activations); 128: one per 128 x 128 tile, written for each of
+ *              its rows (weights).
+ *   svdcache_residual_rmsnorm_fp8   h = H + X;  H_out = h;  y = h * rsqrt(mean(h^2) + eps) * weight;
+ *              Q, S = y in 8 bits, a scale per 1 x 128 group.  fp32 arithmetic, y from the unrounded
+ *              h.  X may be NULL (plain norm), H_out NULL (h not kept) or H itself (in place),
+ *              weight (device, D fp32) NULL for ones.  Needs 8 <= D <= 16384, D % 8 == 0, eps >= 0.
+ *   svdcache_gemm_fp8       C = act(A B^T + bias): A (M x K) and B (N x K) 8-bit with scales SA and
+ *              SB, bias device N fp32 or NULL, act SVDCACHE_ACT_NONE or SVDCACHE_ACT_GELU (tanh
+ *              form).  C (M x N, pitch ldc in ELEMENTS) is F32, BF16 or FP8; FP8 writes its scales
+ *              (a scale per 1 x 128 group) to SC, which is ignored otherwise.  Products are exact,
+ *              sums fp32 in the tensor cores.  1 <= N, K <= 131072.
+ *              status (device, one int32 that the caller sets to 0 once) receives
+ *              SVDCACHE_ERR_TIMEOUT if a bounded in-kernel wait runs out; it is never cleared here.
+ * All three only enqueue work on `stream`.  Results are bit-reproducible.
+ * ------------------------------------------------------------------------------- */
+#define SVDCACHE_ACT_NONE  0
+#define SVDCACHE_ACT_GELU  1   /* x / (1 + exp(-2u)), u = sqrt(2 / pi) (x + 0.044715 x^3) */
+SVDCACHE_API int svdcache_fp8_scale_bytes(int64_t rows, int cols, size_t *bytes /* host, out */);
+SVDCACHE_API int svdcache_quantize_fp8(const void *X, int64_t rows, int cols, int64_t ld, int dtype, int tile_rows,
+                          void *Q, int64_t ldq, void *S, void *stream);
+SVDCACHE_API int svdcache_residual_rmsnorm_fp8(const void *H, int64_t ldh, const void *X, int64_t ldx, void *H_out,
+                                  int64_t ldo, const float *weight, float eps, void *Q, int64_t ldq,
+                                  void *S, int64_t rows, int D, int dtype, void *stream);
+SVDCACHE_API int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb,
+                      const void *SB, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
+                      void *SC, int64_t M, int N, int K, int32_t *status, void *stream);
 
 /* ---------------------------------------------------------------------------------
  * Introspection for benchmarks and tests (host only).

@@ -11,7 +11,7 @@ from typing import Optional, Tuple
 
 import torch
 
-F32, BF16 = 0, 1
+F32, BF16, FP8 = 0, 1, 2
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -65,6 +65,11 @@ SIGNATURES = {
     "svdcache_basis_similarity": (_ci, [_vp, _vp, _vp, _vp, _ci, _ci, _vp, ctypes.POINTER(ctypes.c_double), _vp]),
     "svdcache_singular_values": (_ci, [_vp, _ci, _vp, _vp]),
     "svdcache_left_factors": (_ci, [_vp, _vp, _i64, _ci, _vp, _vp]),
+    "svdcache_fp8_scale_bytes": (_ci, [_i64, _ci, _szp]),
+    "svdcache_quantize_fp8": (_ci, [_vp, _i64, _ci, _i64, _ci, _ci, _vp, _i64, _vp, _vp]),
+    "svdcache_residual_rmsnorm_fp8": (_ci, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, ctypes.c_float, _vp, _i64, _vp, _i64,
+                                            _ci, _ci, _vp]),
+    "svdcache_gemm_fp8": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp]),
 }
 
 
@@ -413,6 +418,125 @@ def svdcache_left_factors(C: torch.Tensor, sigma: torch.Tensor, stream=None) -> 
     U = torch.empty_like(C)
     _check(lib().svdcache_left_factors(_ptr(C), _ptr(sigma), N, k, _ptr(U), _stream(stream)), "left_factors")
     return U
+
+
+# ------------------------------------------------------------- 8-bit linear path ---
+
+ACT_NONE, ACT_GELU = 0, 1
+_BYTES = (torch.uint8, torch.float8_e4m3fn)
+_gemm_status = {}
+
+
+def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().svdcache_fp8_scale_bytes(rows, cols, ctypes.byref(out)), "fp8_scale_bytes")
+    return out.value
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """(pointer, row pitch in elements) of a device matrix whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError(f"{what}: a device matrix with contiguous rows is expected")
+    if t.shape[0] == 1:   # torch gives a single row any stride
+        return t.data_ptr(), -(-t.shape[1] // 16) * 16
+    return t.data_ptr(), t.stride(0)
+
+
+def _fp8_matrix(q: torch.Tensor, s: torch.Tensor, rows: int, cols: int, what: str):
+    if q.dtype not in _BYTES or q.shape[0] != rows or q.shape[1] < cols:
+        raise ValueError(f"{what}: {rows} x {cols} bytes are expected")
+    if not s.is_cuda or s.element_size() != 1 or not s.is_contiguous() or s.numel() < -(-rows // 128) * -(-cols // 512) * 512:
+        raise ValueError(f"{what}: a scale buffer of svdcache_fp8_scale_bytes({rows}, {cols}) bytes is expected")
+    return _matrix(q, what)
+
+
+def svdcache_quantize_fp8(X: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, tile_rows: int = 1, stream=None) -> None:
+    """X [rows, cols] fp32 or bf16 -> e4m3 bytes Q [rows, >= cols] and their scales S (see new_fp8); one scale per
+    1 x 128 group, or with tile_rows = 128 per 128 x 128 tile."""
+    rows, cols = X.shape
+    x, ld = _matrix(X, "X")
+    q, ldq = _fp8_matrix(Q, S, rows, cols, "Q")
+    _check(lib().svdcache_quantize_fp8(x, rows, cols, ld, _dt(X), tile_rows, q, ldq, S.data_ptr(), _stream(stream)),
+           "quantize_fp8")
+
+
+def svdcache_residual_rmsnorm_fp8(H: torch.Tensor, X: Optional[torch.Tensor], H_out: Optional[torch.Tensor],
+                                  weight: Optional[torch.Tensor], eps: float, Q: torch.Tensor, S: torch.Tensor,
+                                  stream=None) -> None:
+    """h = H + X (X None: h = H) -> H_out (None: not kept; H itself: in place); RMS norm of h times weight [D] fp32
+    (None: ones) as an 8-bit matrix Q, S."""
+    rows, D = H.shape
+    h, ldh = _matrix(H, "H")
+    x = ldx = o = ldo = w = None
+    for t, what in ((X, "X"), (H_out, "H_out")):
+        if t is not None and (t.shape != H.shape or t.dtype != H.dtype):
+            raise ValueError(f"{what}: H's shape and type are expected")
+    if X is not None:
+        x, ldx = _matrix(X, "X")
+    if H_out is not None:
+        o, ldo = _matrix(H_out, "H_out")
+    if weight is not None:
+        if weight.dtype != torch.float32 or weight.shape != (D,) or not weight.is_cuda or not weight.is_contiguous():
+            raise ValueError("weight: D fp32 values on the device are expected")
+        w = weight.data_ptr()
+    q, ldq = _fp8_matrix(Q, S, rows, D, "Q")
+    _check(lib().svdcache_residual_rmsnorm_fp8(h, ldh, x, ldx or 0, o, ldo or 0, w, eps, q, ldq, S.data_ptr(), rows, D,
+                                               _dt(H), _stream(stream)), "residual_rmsnorm_fp8")
+
+
+def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: torch.Tensor, K: int, C: torch.Tensor,
+                      S_out: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+                      status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """C [M, N] = act(A B^T + bias) of the 8-bit matrices A [M, >= K] and B [N, >= K].  C is fp32 or bf16, or bytes
+    (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
+    one per device, which gemm_status() reads."""
+    M, N = C.shape
+    a, lda = _fp8_matrix(A, SA, M, K, "A")
+    b, ldb = _fp8_matrix(B, SB, N, K, "B")
+    sc = bi = None
+    if C.dtype in _BYTES:
+        if S_out is None:
+            raise ValueError("S_out: an 8-bit C needs a scale buffer")
+        out, sc = FP8, S_out.data_ptr()
+        c, ldc = _fp8_matrix(C, S_out, M, N, "C")
+    else:
+        out = _dt(C)
+        c, ldc = _matrix(C, "C")
+    if bias is not None:
+        if bias.dtype != torch.float32 or bias.shape != (N,) or not bias.is_cuda or not bias.is_contiguous():
+            raise ValueError("bias: N fp32 values on the device are expected")
+        bi = bias.data_ptr()
+    if status is None:
+        status = _gemm_status.get(C.device)
+        if status is None:
+            status = _gemm_status[C.device] = torch.zeros(1, dtype=torch.int32, device=C.device)
+            torch.cuda.synchronize(C.device)   # the zero is there whatever stream the product runs on
+    _check(lib().svdcache_gemm_fp8(a, lda, SA.data_ptr(), b, ldb, SB.data_ptr(), bi, act, c, ldc, out, sc, M, N, K,
+                                   status.data_ptr(), _stream(stream)), "gemm_fp8")
+
+
+def gemm_status(device="cuda") -> int:
+    """The sticky status of the products on `device` that were given no status word (synchronises): 0, or -6 if a
+    bounded wait ran out in one of them."""
+    device = torch.device(device)
+    if device.index is None:
+        device = torch.device(device.type, torch.cuda.current_device())
+    torch.cuda.synchronize(device)
+    status = _gemm_status.get(device)
+    return 0 if status is None else int(status.item())
+
+
+def new_fp8(rows: int, cols: int, device="cuda"):
+    """Allocate (torch) an 8-bit matrix: bytes [rows, cols up to a multiple of 16] and its scale buffer, zeroed."""
+    q = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=device)
+    return q, torch.zeros(svdcache_fp8_scale_bytes(rows, cols), dtype=torch.uint8, device=device)
+
+
+def fp8_scale_exponents(S: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
+    """The scale bytes of a buffer as [rows, groups of 128 columns] (a copy); scale = 2^(byte - 127)."""
+    i, j, g = -(-rows // 128), -(-cols // 512), -(-cols // 128)
+    pieces = S.view(torch.uint8).reshape(-1)[:i * j * 512].view(i, j, 32, 4, 4)
+    return pieces.permute(0, 3, 2, 1, 4).reshape(128 * i, 4 * j)[:rows, :g]
 
 
 # ---------------------------------------------------------- views for tests/tools ---

@@ -7,6 +7,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "fp8.cuh"
 #include "internal.cuh"
 
 namespace svdc {
@@ -416,6 +417,88 @@ int svdcache_left_factors(const float *C, const double *sigma, int64_t N, int k,
     if (!C || !sigma || !U) return SVDCACHE_ERR_INVALID_ARG;
     if (N < 1 || k < 1 || k > 16384) return SVDCACHE_ERR_BAD_SHAPE;
     return left_factors_launch(C, sigma, N, k, U, (cudaStream_t)stream);
+}
+
+/* ----------------------------------------------------------- 8-bit linear path --- */
+
+static const int64_t kFp8MaxRows = 0x7FFFFFFFLL - 256;
+static const int kFp8MaxCols = 131072;
+
+static int check_fp8_shape(int64_t rows, int cols) {
+    return rows < 0 || rows >= kFp8MaxRows || cols < 1 || cols > kFp8MaxCols ? SVDCACHE_ERR_BAD_SHAPE : SVDCACHE_OK;
+}
+
+// a matrix of `elem`-byte values: pointer and pitch
+static int check_matrix(const void *p, int64_t ld, int cols, int elem) {
+    if (!p) return SVDCACHE_ERR_INVALID_ARG;
+    if (ld < cols || ld > (1LL << 36)) return SVDCACHE_ERR_BAD_SHAPE;
+    return aligned16(p) && (ld * elem) % 16 == 0 ? SVDCACHE_OK : SVDCACHE_ERR_BAD_ALIGN;
+}
+
+static int check_fp8_matrix(const void *q, int64_t ld, int cols, const void *s) {
+    if (!s) return SVDCACHE_ERR_INVALID_ARG;
+    const int rc = check_matrix(q, ld, cols, 1);
+    return rc ? rc : aligned16(s) ? SVDCACHE_OK : SVDCACHE_ERR_BAD_ALIGN;
+}
+
+int svdcache_fp8_scale_bytes(int64_t rows, int cols, size_t *bytes) {
+    if (!bytes) return SVDCACHE_ERR_INVALID_ARG;
+    const int rc = check_fp8_shape(rows, cols);
+    if (rc) return rc;
+    *bytes = fp8_scale_bytes(rows, cols);
+    return SVDCACHE_OK;
+}
+
+int svdcache_quantize_fp8(const void *X, int64_t rows, int cols, int64_t ld, int dtype, int tile_rows, void *Q,
+                          int64_t ldq, void *S, void *stream) {
+    NvtxRange range("svdcache_quantize_fp8");
+    if ((dtype != SVDCACHE_F32 && dtype != SVDCACHE_BF16) || (tile_rows != 1 && tile_rows != kScaleRows))
+        return SVDCACHE_ERR_INVALID_ARG;
+    int rc = check_fp8_shape(rows, cols);
+    if (rc || rows == 0) return rc;
+    rc = check_matrix(X, ld, cols, (int)elem_bytes(dtype));
+    if (!rc) rc = check_fp8_matrix(Q, ldq, cols, S);
+    if (rc) return rc;
+    return quantize_fp8_launch(X, rows, cols, ld, dtype, tile_rows, Q, ldq, S, (cudaStream_t)stream);
+}
+
+int svdcache_residual_rmsnorm_fp8(const void *H, int64_t ldh, const void *X, int64_t ldx, void *H_out, int64_t ldo,
+                                  const float *weight, float eps, void *Q, int64_t ldq, void *S, int64_t rows, int D,
+                                  int dtype, void *stream) {
+    NvtxRange range("svdcache_residual_rmsnorm_fp8");
+    if ((dtype != SVDCACHE_F32 && dtype != SVDCACHE_BF16) || !(eps >= 0.0f)) return SVDCACHE_ERR_INVALID_ARG;
+    int rc = check_fp8_shape(rows, D);
+    if (rc) return rc;
+    if (D < 8 || D > 16384 || (D % 8) != 0) return SVDCACHE_ERR_BAD_SHAPE;
+    if (rows == 0) return SVDCACHE_OK;
+    rc = check_matrix(H, ldh, D, (int)elem_bytes(dtype));
+    if (!rc && X) rc = check_matrix(X, ldx, D, (int)elem_bytes(dtype));
+    if (!rc && H_out) rc = check_matrix(H_out, ldo, D, (int)elem_bytes(dtype));
+    if (!rc) rc = check_fp8_matrix(Q, ldq, D, S);
+    if (!rc && weight && !aligned16(weight)) rc = SVDCACHE_ERR_BAD_ALIGN;
+    if (rc) return rc;
+    return rmsnorm_fp8_launch(H, ldh, X, ldx, H_out, ldo, weight, eps, Q, ldq, S, rows, D, dtype, (cudaStream_t)stream);
+}
+
+int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
+                      const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
+                      int32_t *status, void *stream) {
+    NvtxRange range("svdcache_gemm_fp8");
+    if (act != SVDCACHE_ACT_NONE && act != SVDCACHE_ACT_GELU) return SVDCACHE_ERR_INVALID_ARG;
+    if (out_dtype != SVDCACHE_F32 && out_dtype != SVDCACHE_BF16 && out_dtype != SVDCACHE_FP8) return SVDCACHE_ERR_INVALID_ARG;
+    int rc = check_fp8_shape(M, K);
+    if (!rc) rc = check_fp8_shape(M, N);
+    if (rc || M == 0) return rc;
+    if (!status) return SVDCACHE_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(status) & 3u) || (reinterpret_cast<uintptr_t>(bias) & 3u)) return SVDCACHE_ERR_BAD_ALIGN;
+    rc = check_fp8_matrix(A, lda, K, SA);
+    if (!rc) rc = check_fp8_matrix(B, ldb, K, SB);
+    if (!rc) rc = out_dtype == SVDCACHE_FP8 ? check_fp8_matrix(C, ldc, N, SC) : check_matrix(C, ldc, N, (int)elem_bytes(out_dtype));
+    if (rc) return rc;
+    GemmFp8Args a{};
+    a.A = A; a.B = B; a.SA = SA; a.SB = SB; a.lda = lda; a.ldb = ldb; a.ldc = ldc; a.bias = bias; a.C = C; a.SC = SC;
+    a.M = M; a.N = N; a.K = K; a.act = act; a.out = out_dtype; a.status = status;
+    return gemm_fp8_launch(a, (cudaStream_t)stream);
 }
 
 /* Blocks of different rank in one call: consecutive blocks of equal rank form one batched launch. */

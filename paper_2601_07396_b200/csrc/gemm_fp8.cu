@@ -1,0 +1,332 @@
+// Matrix product of two 8-bit matrices (format: fp8.cuh) on the tensor cores of sm_100a:
+//     C[m, n] = act( sum_g sA[m, g] sB[n, g] sum_{k in g} A[m, k] B[n, k]  +  bias[n] )
+// with act the identity or gelu(x) = x / (1 + exp(-2u)), u = sqrt(2 / pi) (x + 0.044715 x^3) (the tanh form), and
+// C in fp32, bf16 or 8 bits again with a scale per row and 128 columns.  The scales are powers of two, so
+// kind::mxf8f6f4 applies them: an MMA of K = 32 takes one scale byte per row of either operand, and a piece of
+// 128 rows x 4 groups reaches tensor memory as it is stored (tcgen05.cp), one word per row whose byte g % 4 the
+// four MMAs of group g name.  Sums are fp32 in tensor memory.
+//
+// tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns are up to 256 rows of
+// C, so that few rows of C waste no tensor work.  One CTA per tile and K range; the CTAs of a cluster share a
+// tile, each sums its own K range, and after one cluster barrier each adds up its share of the rows over the
+// cluster in rank order (distributed shared memory): no atomics, the same sum in every run.
+// Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
+#include "fp8.cuh"
+#include "umma.cuh"
+
+namespace svdc {
+
+using namespace sm100;
+
+namespace {
+
+constexpr int kTileN = 128;                           // columns of C per tile: MMA M
+constexpr int kStageK = 128;                          // bytes of K per pipeline stage: one scale group
+constexpr uint32_t kBBytes = kTileN * kStageK;
+constexpr int kTileThreads = 192;
+constexpr int kMaxStages = 12;
+
+struct TileParams {
+    int64_t M, ldc;
+    int N, K, groups, splits, n_tiles, tile_m, stages, tmem_cols;
+    int64_t pieces;                 // scale pieces along K
+    uint32_t a_bytes, stage_bytes;
+    const uint8_t *SA, *SB;
+    const float *bias;
+    void *C;
+    uint8_t *SC;
+    int64_t pieces_c;
+    int act, out;
+    int *status;
+};
+
+__device__ __forceinline__ float gelu_tanh(float x) {
+    const float u = 0.7978845608f * fmaf(0.044715f * x * x, x, x);
+    return x / (1.0f + __expf(-2.0f * u));
+}
+
+// four neighbouring columns n .. n + 3 of row m of C (n a multiple of 4): plain types
+__device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int n, const float (&v)[4]) {
+    if (p.out == SVDCACHE_F32) {
+        float *o = reinterpret_cast<float *>(p.C) + m * p.ldc + n;
+        if (n + 4 <= p.N) *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            for (int i = 0; i < 4; ++i)
+                if (n + i < p.N) o[i] = v[i];
+    } else {
+        __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(p.C) + m * p.ldc + n;
+        if (n + 4 <= p.N) {
+            const __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+            *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<const uint2 *>(w);
+        } else {
+            for (int i = 0; i < 4; ++i)
+                if (n + i < p.N) o[i] = __float2bfloat16_rn(v[i]);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kTileThreads)
+tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const TileParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxStages + 1];
+    __shared__ uint32_t tmem_slot_mem;
+    __shared__ int abort_mem;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    float *stage_f32 = reinterpret_cast<float *>(smem_raw + (base - smem_u32(smem_raw)));
+    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxStages, done_bar = empty + 8 * kMaxStages;
+    volatile int *abort_flag = &abort_mem;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    const int rank = (int)(blockIdx.x % (unsigned)p.splits);            // = rank in the cluster
+    const int tile = (int)(blockIdx.x / (unsigned)p.splits);
+    const int n_tile = tile % p.n_tiles;
+    const int64_t m0 = (int64_t)(tile / p.n_tiles) * p.tile_m;
+    const int n0 = n_tile * kTileN;
+    const int g_lo = (int)((int64_t)p.groups * rank / p.splits), g_hi = (int)((int64_t)p.groups * (rank + 1) / p.splits);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        mbar_init(done_bar, 1);
+        abort_mem = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tm_a);
+        prefetch_tensormap(&tm_b);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&tmem_slot_mem), (uint32_t)p.tmem_cols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 1;
+            const int64_t piece_a = m0 / kScaleRows, last_a = (p.M - 1) / kScaleRows;
+            for (int g = g_lo; g < g_hi; ++g) {
+                if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) break;
+                const uint32_t dst = base + s * p.stage_bytes, bar = full + 8 * s;
+                const bool scales = g == g_lo || (g & (kScaleGroups - 1)) == 0;
+                const int na = scales ? (p.tile_m > kScaleRows && piece_a + 1 <= last_a ? 2 : 1) : 0;
+                mbar_arrive_expect_tx(bar, kBBytes + p.a_bytes + (scales ? (1 + na) * kScalePieceBytes : 0));
+                tma_load_2d(dst, &tm_b, bar, g * kStageK, n0);
+                tma_load_2d(dst + kBBytes, &tm_a, bar, g * kStageK, (int)m0);
+                if (scales) {
+                    const uint32_t sdst = dst + kBBytes + p.a_bytes;
+                    const int64_t at = g / kScaleGroups;
+                    bulk_load(sdst, p.SB + ((size_t)n_tile * p.pieces + at) * kScalePieceBytes, kScalePieceBytes, bar);
+                    for (int i = 0; i < na; ++i)
+                        bulk_load(sdst + (1 + i) * kScalePieceBytes, p.SA + ((size_t)(piece_a + i) * p.pieces + at) * kScalePieceBytes,
+                                  kScalePieceBytes, bar);
+                }
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            // scale words: four columns for B, then eight for A; two sets that alternate
+            const uint32_t sf = tmem + (uint32_t)p.tmem_cols - 32u;
+            const uint32_t a_word = (uint32_t)(m0 % kScaleRows) / 32u;   // a tile of fewer than 128 rows may begin inside a piece
+            uint32_t set = 1;
+            for (int g = g_lo; g < g_hi; ++g) {
+                if (!mbar_wait(full + 8 * s, ph, abort_flag, 2)) break;
+                tc_fence_after();
+                const uint32_t src = base + s * p.stage_bytes;
+                if (g == g_lo || (g & (kScaleGroups - 1)) == 0) {
+                    set ^= 1u;
+                    const uint32_t ssrc = src + kBBytes + p.a_bytes;
+                    tmem_cp_scales(sf + 16 * set, smem_desc_scales(ssrc));
+                    tmem_cp_scales(sf + 16 * set + 4, smem_desc_scales(ssrc + kScalePieceBytes));
+                    if (p.tile_m > kScaleRows) tmem_cp_scales(sf + 16 * set + 8, smem_desc_scales(ssrc + 2 * kScalePieceBytes));
+                }
+                const uint64_t bd = smem_desc_kmajor(src, 128), ad = smem_desc_kmajor(src + kBBytes, 128);
+                const uint32_t idesc = idesc_mxf8(kTileN, p.tile_m, g & 3);
+#pragma unroll
+                for (int ks = 0; ks < kStageK / 32; ++ks)
+                    mma_mxf8_ss(tmem, bd + 2 * ks, ad + 2 * ks, idesc, sf + 16 * set, sf + 16 * set + 4 + a_word,
+                                (g > g_lo || ks > 0) ? 1u : 0u);
+                mma_commit(empty + 8 * s);
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+            mma_commit(done_bar);
+        }
+        __syncwarp();
+    } else {
+        // accumulator -> shared memory, [row of C][128 columns]: the ring is free once every MMA is done
+        const int q = warp & 3;
+        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(done_bar, 0u, abort_flag, 3));
+        tc_fence_after();
+        if (ok && g_hi > g_lo) {
+            for (int c = 0; c < p.tile_m; c += 32) {
+                uint32_t acc[32];
+                tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + c, acc);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (c + i < p.tile_m) stage_f32[(c + i) * kTileN + q * 32 + lane] = __uint_as_float(acc[i]);
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (*abort_flag) {
+        // a wait ran out: tell the host, and let what is in flight land before the memory goes
+        if (threadIdx.x == 0) {
+            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
+            const long long t0 = clock64();
+            while (clock64() - t0 < kWaitCycles / 100) {}
+        }
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+    }
+    if (p.splits > 1) cluster_sync();
+
+    // rows of the tile are dealt to the cluster's CTAs in equal runs, a warp per row, four columns per lane
+    const int per = (p.tile_m + p.splits - 1) / p.splits, r_lo = rank * per;
+    const int r_hi = min(min(r_lo + per, p.tile_m), (int)(p.M - m0 < p.tile_m ? p.M - m0 : p.tile_m));
+    const int n = n0 + 4 * lane;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (p.bias)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.N) bias[i] = p.bias[n + i];
+    for (int r = r_lo + warp; r < r_hi; r += kTileThreads / 32) {
+        const uint32_t at = base + (uint32_t)(r * kTileN + 4 * lane) * 4u;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < p.splits; ++x) {
+            const float4 w = cluster_load(cluster_addr(at, (uint32_t)x));
+            v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] += bias[i];
+            if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
+        }
+        const int64_t m = m0 + r;
+        if (p.out != SVDCACHE_FP8) {
+            store_plain(p, m, n, v);
+            continue;
+        }
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = n + i < p.N ? fp8_nan_if_not_finite(v[i]) : 0.0f;
+            top = fmaxf(top, fabsf(v[i]));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const uint32_t byte = fp8_scale_byte(top);
+        const float inv = fp8_inverse_scale(byte);
+        const uint32_t w = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        uint8_t *o = reinterpret_cast<uint8_t *>(p.C) + m * p.ldc + n;
+        if (n + 4 <= p.N) *reinterpret_cast<uint32_t *>(o) = w;
+        else
+            for (int i = 0; i < 4; ++i)
+                if (n + i < p.N) o[i] = (uint8_t)(w >> (8 * i));
+        if (lane == 0) p.SC[fp8_scale_offset(m, n_tile, p.pieces_c)] = (uint8_t)byte;
+    }
+    if (p.splits > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
+}
+
+// ------------------------------------------------------------------------- host side ---
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = [] {
+        void *ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiledFn>(ptr);
+        return (EncodeTiledFn) nullptr;
+    }();
+    return fn;
+}
+
+// bytes [rows x cols], rows `ld` bytes apart, boxes of 128 bytes x box_rows with the 128-byte swizzle; bytes
+// beyond the matrix read as zero, which is e4m3's zero
+int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t ld, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return SVDCACHE_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kStageK, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
+}
+
+int sm_count() {
+    int dev = 0, n = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    return n > 0 ? n : 148;
+}
+
+constexpr size_t kSmemBudget = 225 * 1024;   // of 227 KB: the barriers are static
+
+int tile_launch(const GemmFp8Args &a, cudaStream_t s) {
+    TileParams p{};
+    p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
+    p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
+    p.act = a.act; p.out = a.out; p.status = a.status;
+    p.groups = (int)fp8_groups(a.K); p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
+    p.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    p.n_tiles = (a.N + kTileN - 1) / kTileN;
+    const int64_t tiles = (a.M + p.tile_m - 1) / p.tile_m * p.n_tiles;
+    p.splits = 1;
+    while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.groups >= 2 * p.splits) p.splits *= 2;
+    if (tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    p.a_bytes = (uint32_t)p.tile_m * kStageK;
+    p.stage_bytes = kBBytes + p.a_bytes + (p.a_bytes < 1024 * 32 ? 1024u : 2048u);
+    p.tmem_cols = p.tile_m <= 32 ? 64 : p.tile_m == 64 ? 128 : p.tile_m == 128 ? 256 : 512;
+    int stages = (int)((kSmemBudget - 1024) / p.stage_bytes);
+    if (stages > kMaxStages) stages = kMaxStages;
+    const int longest = (p.groups + p.splits - 1) / p.splits;
+    const int least = (int)(((size_t)p.tile_m * kTileN * 4 + p.stage_bytes - 1) / p.stage_bytes);   // the accumulator passes through the ring
+    if (stages > longest) stages = longest > least ? longest : least;
+    p.stages = stages;
+    const size_t smem = 1024 + (size_t)stages * p.stage_bytes;
+
+    CUtensorMap tm_a, tm_b;
+    int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
+    if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, kTileN);
+    if (!rc) rc = record_cuda(cudaFuncSetAttribute(tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (rc) return rc;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles * p.splits));
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    rc = record_cuda(cudaLaunchKernelEx(&cfg, tile_kernel, tm_a, tm_b, p));
+    if (rc) return rc;
+    count_launch();
+    return check_last_launch();
+}
+
+}  // namespace
+
+int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) { return tile_launch(a, s); }
+
+}  // namespace svdc
