@@ -11,6 +11,8 @@
 // tile, each sums its own K range, and after one cluster barrier each adds up its share of the rows over the
 // cluster in rank order (distributed shared memory): no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
+#include <type_traits>
+
 #include "fp8.cuh"
 #include "umma.cuh"
 
@@ -237,6 +239,319 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     if (p.splits > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
 }
 
+// ---------------------------------------------------------------------- pairs of CTAs ---
+//
+// pair_kernel: a persistent cluster of two CTAs computes tiles of 256 x 256 of C with cta_group::2 MMAs: each CTA
+// holds 128 rows of the tile in its tensor memory and loads its 128 rows of A and half of the tile's rows of B, so
+// a group of K costs an SM 32 KB instead of the 48 KB of a one-CTA 128 x 256 tile -- the traffic between L2 and
+// the SMs is what bounds such a kernel first.
+// Tensor memory (512 columns): two accumulators of 256 columns that share 32, columns [0, 256) and [224, 480), and
+// two sets of scale words in the last 32.  The epilogue reads the shared columns first, and the MMAs of the next
+// tile start as soon as they are read.
+// Warps: 0 TMA producer, 1 MMA issuer (the first CTA's, for both), 2-5 and 6-9 the two column halves of the tile.
+
+constexpr int kPairM = 256, kPairN = 256;
+constexpr int kPairThreads = 320;
+constexpr int kPairStages = 5;
+constexpr uint32_t kPairABytes = 128 * kStageK, kPairBBytes = 128 * kStageK;      // each CTA's share
+constexpr uint32_t kPairScaleBytes = 3 * kScalePieceBytes;                        // own rows of A, all 256 of B
+constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes + 2048;
+constexpr uint32_t kStoreBytes = 32 * 128;                                        // a warp's box of C: 32 rows of 128 bytes
+constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStageBytes + 8 * kStoreBytes;
+constexpr uint32_t kAccStep = 224, kScaleCol = 480;
+constexpr int kRasterRows = 8;      // tile rows that neighbouring clusters share: 8 x n tiles are walked column by column
+
+struct PairParams {
+    int64_t M, ldc;
+    void *C;
+    int N, groups, m_tiles, n_tiles, tiles;
+    const float *bias;
+    uint8_t *SC;
+    int64_t pieces_c;
+    int act;
+    int *status;
+};
+
+struct TileAt { int m, n; };
+__device__ __forceinline__ TileAt pair_tile(const PairParams &p, int t) {
+    const int band = kRasterRows * p.n_tiles, b = t / band, in = t - b * band;
+    const int rows = min(kRasterRows, p.m_tiles - b * kRasterRows);
+    return {b * kRasterRows + in % rows, in / rows};
+}
+
+// A warp's box of C (32 rows of 128 bytes, 16-byte pieces swizzled), written by all its lanes, on its way out.  A TMA
+// store ends at a multiple of 16 bytes, not at the matrix's last column: a box that the last column cuts elsewhere is
+// written by the lanes, so that nothing beyond column N changes.
+template <typename T>
+__device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairParams &p, uint32_t box, int n, int64_t row0, int lane) {
+    constexpr int kCols = 128 / (int)sizeof(T);
+    if (n >= p.N || row0 >= p.M) return;
+    if (n + kCols <= p.N || (p.N * (int)sizeof(T)) % 16 == 0) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(tm_c, box, n, (int)row0);
+            tma_store_commit();
+        }
+        return;
+    }
+    __syncwarp();
+    for (int r = 0; r < 32 && row0 + r < p.M; ++r) {
+        T *out = reinterpret_cast<T *>(p.C) + (row0 + r) * p.ldc + n;
+        for (int c = lane; c < p.N - n; c += 32) {
+            const uint32_t byte = (uint32_t)c * sizeof(T);
+            const uint32_t at = box + (uint32_t)r * 128u + ((byte >> 4) ^ (uint32_t)(r & 7)) * 16u + (byte & 15u);
+            if constexpr (sizeof(T) == 4) asm volatile("{.reg .b32 v; ld.shared.b32 v, [%1]; st.global.b32 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
+            else if constexpr (sizeof(T) == 2) asm volatile("{.reg .b16 v; ld.shared.b16 v, [%1]; st.global.b16 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
+            else asm volatile("{.reg .b16 v; ld.shared.b8 v, [%1]; st.global.b8 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
+        }
+    }
+    __syncwarp();
+}
+
+template <int OUT>
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+            const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ CUtensorMap tm_sb,
+            const __grid_constant__ CUtensorMap tm_c, const PairParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) unsigned long long bar_mem[2 * kPairStages + 2];
+    __shared__ __align__(16) float bias_mem[8][kPairN / 2];
+    __shared__ uint32_t tmem_slot_mem;
+    __shared__ int abort_mem;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kPairStages, acc_full = empty + 8 * kPairStages, acc_empty = acc_full + 8;
+    volatile int *abort_flag = &abort_mem;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x & 1u;           // in the cluster
+    const int cluster = (int)(blockIdx.x >> 1), clusters = (int)(gridDim.x >> 1);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 16);                    // the epilogue warps of both CTAs
+        abort_mem = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tm_a);
+        prefetch_tensormap(&tm_b);
+        prefetch_tensormap(&tm_sa);
+        prefetch_tensormap(&tm_sb);
+        prefetch_tensormap(&tm_c);
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(smem_u32(&tmem_slot_mem), 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                  // both CTAs' barriers exist
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t ph = 1;
+            for (int t = cluster; t < p.tiles; t += clusters) {
+                const TileAt at = pair_tile(p, t);
+                const int row_a = at.m * kPairM + (int)rank * 128, row_b = at.n * kPairN + (int)rank * 128;
+                for (int g = 0; g < p.groups; ++g) {
+                    if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) goto done;
+                    const uint32_t dst = base + s * kPairStageBytes, bar = cluster_addr(full + 8 * s, 0);
+                    const bool scales = (g & (kScaleGroups - 1)) == 0;
+                    if (rank == 0)
+                        mbar_arrive_expect_tx(full + 8 * s, 2 * (kPairABytes + kPairBBytes + (scales ? kPairScaleBytes : 0)));
+                    tma_load_2d_pair(dst, &tm_a, bar, g * kStageK, row_a);
+                    tma_load_2d_pair(dst + kPairABytes, &tm_b, bar, g * kStageK, row_b);
+                    if (scales) {
+                        // the scale buffers as rows of pieces, g / 4 the piece of the row
+                        const uint32_t sdst = dst + kPairABytes + kPairBBytes;
+                        const int c = g / kScaleGroups * (kScalePieceBytes / 4);
+                        tma_load_2d_pair(sdst, &tm_sa, bar, c, at.m * 2 + (int)rank);
+                        tma_load_2d_pair(sdst + kScalePieceBytes, &tm_sb, bar, c, at.n * 2);
+                        tma_load_2d_pair(sdst + 2 * kScalePieceBytes, &tm_sb, bar, c, at.n * 2 + 1);
+                    }
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            int s = 0;
+            uint32_t ph = 0, it = 0, set = 1;
+            for (int t = cluster; t < p.tiles; t += clusters, ++it) {
+                if (it > 0 && !mbar_wait(acc_empty, (it - 1) & 1u, abort_flag, 2)) goto done;
+                tc_fence_after();
+                const uint32_t acc = tmem + (it & 1u) * kAccStep;
+                for (int g = 0; g < p.groups; ++g) {
+                    if (!mbar_wait(full + 8 * s, ph, abort_flag, 3)) goto done;
+                    tc_fence_after();
+                    const uint32_t src = base + s * kPairStageBytes;
+                    if ((g & (kScaleGroups - 1)) == 0) {
+                        set ^= 1u;
+                        const uint32_t ssrc = src + kPairABytes + kPairBBytes, sf = tmem + kScaleCol + 16 * set;
+                        tmem_cp_scales_pair(sf, smem_desc_scales(ssrc));
+                        tmem_cp_scales_pair(sf + 4, smem_desc_scales(ssrc + kScalePieceBytes));
+                        tmem_cp_scales_pair(sf + 8, smem_desc_scales(ssrc + 2 * kScalePieceBytes));
+                    }
+                    const uint32_t sf = tmem + kScaleCol + 16 * set;
+                    const uint64_t ad = smem_desc_kmajor(src, 128), bd = smem_desc_kmajor(src + kPairABytes, 128);
+                    const uint32_t idesc = idesc_mxf8(kPairM, kPairN, g & 3);
+#pragma unroll
+                    for (int ks = 0; ks < kStageK / 32; ++ks)
+                        mma_mxf8_ss_pair(acc, ad + 2 * ks, bd + 2 * ks, idesc, sf, sf + 4, (g > 0 || ks > 0) ? 1u : 0u);
+                    mma_commit_pair(empty + 8 * s);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+                mma_commit_pair(acc_full);
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t store = base + kPairStages * kPairStageBytes + (uint32_t)(warp - 2) * kStoreBytes;
+        const uint32_t store_row = store + (uint32_t)lane * 128u;
+        float *bias = bias_mem[warp - 2];
+        const uint32_t acc_empty_first = cluster_addr(acc_empty, 0);
+        constexpr int kCols = OUT == SVDCACHE_FP8 ? 128 : OUT == SVDCACHE_BF16 ? 64 : 32;   // columns of C in 128 bytes
+        uint32_t it = 0;
+        for (int t = cluster; t < p.tiles; t += clusters, ++it) {
+            const TileAt at = pair_tile(p, t);
+            const int64_t row0 = (int64_t)at.m * kPairM + rank * 128 + q * 32;
+            const int col0 = at.n * kPairN + half * 128;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = col0 + j * 32 + lane;
+                bias[j * 32 + lane] = p.bias && n < p.N ? p.bias[n] : 0.0f;
+            }
+            __syncwarp();
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full, it & 1u, abort_flag, 4))) goto done;
+            tc_fence_after();
+            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (it & 1u) * kAccStep + half * 128;
+            // the columns that the next accumulator shares: the last 32 of the first one, the first 32 of the second
+            const bool shares = half == (int)((it & 1u) ^ 1u);
+            if (!shares && lane == 0) mbar_arrive_cluster(acc_empty_first);
+            // column blocks of 32, the shared one first
+            const int first = shares && half == 1 ? 3 : 0;
+            if constexpr (OUT == SVDCACHE_FP8) {
+                float v[128];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t r[32];
+                    tmem_ld_32x32(acc + j * 32, r);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[j * 32 + i] = __uint_as_float(r[i]);
+                }
+                tmem_wait_ld();
+                tc_fence_before();
+                if (shares) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(acc_empty_first);
+                }
+                float top = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 128; ++i) {
+                    v[i] += bias[i];
+                    if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
+                    v[i] = col0 + i < p.N ? v[i] : 0.0f;
+                    top = fmaxf(top, fabsf(v[i]));
+                }
+                if (__float_as_uint(top) == 0x7F800000u) {
+                    top = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) {
+                        v[i] = fp8_nan_if_not_finite(v[i]);
+                        top = fmaxf(top, fabsf(v[i]));
+                    }
+                }
+                const uint32_t byte = fp8_scale_byte(top);
+                const float inv = fp8_inverse_scale(byte);
+                if (lane == 0) tma_store_wait_read<0>();      // the last box has left
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int k = c * 16 + i * 4;
+                        w[i] = fp8_pack4(v[k] * inv, v[k + 1] * inv, v[k + 2] * inv, v[k + 3] * inv);
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                 ::"r"(store_row + (uint32_t)(c ^ (lane & 7)) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                if (row0 + lane < p.M && col0 < p.N) p.SC[fp8_scale_offset(row0 + lane, col0 / kFp8Group, p.pieces_c)] = (uint8_t)byte;
+                send_box<uint8_t>(&tm_c, p, store, col0, row0, lane);
+            } else {
+#pragma unroll 1
+                for (int jj = 0; jj < 4; ++jj) {
+                    // bf16 boxes hold two blocks: 0 1 | 2 3, or 3 2 | 1 0
+                    const int j = first ? 3 - jj : jj;
+                    uint32_t r[32];
+                    tmem_ld_32x32(acc + j * 32, r);
+                    tmem_wait_ld();
+                    if (jj == 0 && shares) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(acc_empty_first);
+                    }
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        v[i] = __uint_as_float(r[i]) + bias[j * 32 + i];
+                        if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
+                    }
+                    constexpr int kBlocks = kCols / 32;       // blocks per box
+                    if (jj % kBlocks == 0) {
+                        if (lane == 0) tma_store_wait_read<0>();
+                        __syncwarp();
+                    }
+                    const int c0 = kBlocks == 2 ? (j & 1) * 4 : 0;
+#pragma unroll
+                    for (int c = 0; c < 8 / kBlocks; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (OUT == SVDCACHE_BF16) {
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(v[c * 8 + 2 * i], v[c * 8 + 2 * i + 1]);
+                                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+                            } else {
+                                w[i] = __float_as_uint(v[c * 4 + i]);
+                            }
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                     ::"r"(store_row + (uint32_t)((c0 + c) ^ (lane & 7)) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                    if (jj % kBlocks == kBlocks - 1) {
+                        send_box<typename std::conditional<OUT == SVDCACHE_BF16, __nv_bfloat16, float>::type>(
+                            &tm_c, p, store, col0 + j / kBlocks * kCols, row0, lane);
+                    }
+                }
+                tc_fence_before();
+            }
+        }
+        if (lane == 0) tma_store_wait<0>();
+    }
+
+done:
+    __syncwarp();
+    __syncthreads();
+    if (*abort_flag) {
+        // a wait ran out: tell the host, and let what is in flight land before the memory goes
+        if (threadIdx.x == 0) {
+            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
+            const long long t0 = clock64();
+            while (clock64() - t0 < kWaitCycles / 100) {}
+        }
+        __syncthreads();
+    }
+    tc_fence_before();
+    cluster_sync();      // neither CTA signals the other any more
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem, 512);
+    }
+}
+
 // ------------------------------------------------------------------------- host side ---
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -325,8 +640,70 @@ int tile_launch(const GemmFp8Args &a, cudaStream_t s) {
     return check_last_launch();
 }
 
+// a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
+// the buffer read as zero.
+int scale_map(CUtensorMap *m, const void *base, int64_t rows, int64_t pieces) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return SVDCACHE_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)pieces * (kScalePieceBytes / 4), (cuuint64_t)((rows + kScaleRows - 1) / kScaleRows)};
+    const cuuint64_t strides[1] = {(cuuint64_t)pieces * kScalePieceBytes};
+    const cuuint32_t box[2] = {kScalePieceBytes / 4, 1};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, const_cast<void *>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
+}
+
+// C in boxes of 32 rows x 128 bytes; what lies beyond M or N is not written
+int out_map(CUtensorMap *m, const GemmFp8Args &a) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return SVDCACHE_ERR_CUDA;
+    const int elem = a.out == SVDCACHE_FP8 ? 1 : a.out == SVDCACHE_BF16 ? 2 : 4;
+    const CUtensorMapDataType t = a.out == SVDCACHE_FP8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                  : a.out == SVDCACHE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    const cuuint64_t dims[2] = {(cuuint64_t)a.N, (cuuint64_t)a.M};
+    const cuuint64_t strides[1] = {(cuuint64_t)a.ldc * elem};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / elem), 32};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(m, t, 2, a.C, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
+}
+
+int pair_launch(const GemmFp8Args &a, cudaStream_t s) {
+    PairParams p{};
+    p.M = a.M; p.N = a.N; p.groups = (int)fp8_groups(a.K); p.C = a.C; p.ldc = a.ldc;
+    p.n_tiles = (a.N + kPairN - 1) / kPairN;
+    const int64_t m_tiles = (a.M + kPairM - 1) / kPairM;
+    if (m_tiles * p.n_tiles > 0x3FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    p.m_tiles = (int)m_tiles;
+    p.tiles = p.m_tiles * p.n_tiles;
+    p.bias = a.bias; p.SC = (uint8_t *)a.SC; p.pieces_c = fp8_piece_cols(a.N); p.act = a.act; p.status = a.status;
+    CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_c;
+    int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, 128);
+    if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, 128);
+    if (!rc) rc = scale_map(&tm_sa, a.SA, a.M, fp8_piece_cols(a.K));
+    if (!rc) rc = scale_map(&tm_sb, a.SB, a.N, fp8_piece_cols(a.K));
+    if (!rc) rc = out_map(&tm_c, a);
+    if (rc) return rc;
+    const int clusters = sm_count() / 2 < p.tiles ? sm_count() / 2 : p.tiles;
+    auto launch = [&](auto kern) {
+        const int e = record_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem));
+        if (e) return e;
+        kern<<<2 * clusters, kPairThreads, kPairSmem, s>>>(tm_a, tm_b, tm_sa, tm_sb, tm_c, p);
+        count_launch();
+        return check_last_launch();
+    };
+    return a.out == SVDCACHE_FP8 ? launch(pair_kernel<SVDCACHE_FP8>)
+           : a.out == SVDCACHE_BF16 ? launch(pair_kernel<SVDCACHE_BF16>) : launch(pair_kernel<SVDCACHE_F32>);
+}
+
 }  // namespace
 
-int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) { return tile_launch(a, s); }
+int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
+    if (a.M > 256 && a.N > 256) return pair_launch(a, s);
+    return tile_launch(a, s);
+}
 
 }  // namespace svdc
