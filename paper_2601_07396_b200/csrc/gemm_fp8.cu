@@ -42,9 +42,14 @@ struct TileParams {
     int *status;
 };
 
+// x / (1 + exp(-2u)) by ex2 and rcp (each good to a few 2^-23): exp(-2u) = 2^(x (a + b x^2)).  Beyond the range of
+// exp the quotient is 0 or x.
 __device__ __forceinline__ float gelu_tanh(float x) {
-    const float u = 0.7978845608f * fmaf(0.044715f * x * x, x, x);
-    return x / (1.0f + __expf(-2.0f * u));
+    const float t = x * fmaf(x * x, -0.10294324f, -2.3022082f);    // -2 sqrt(2 / pi) log2(e) {0.044715, 1}
+    float e, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(t));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return x * r;
 }
 
 // four neighbouring columns n .. n + 3 of row m of C (n a multiple of 4): plain types
@@ -279,6 +284,19 @@ __device__ __forceinline__ TileAt pair_tile(const PairParams &p, int t) {
     return {b * kRasterRows + in % rows, in / rows};
 }
 
+// v += bias (shared memory, the same for every lane), then the activation
+template <int N> __device__ __forceinline__ void add_bias_and_act(float *v, const float *bias, int act) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const float4 b = *reinterpret_cast<const float4 *>(bias + i);
+        v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+    }
+    if (act == SVDCACHE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gelu_tanh(v[i]);
+    }
+}
+
 // A warp's box of C (32 rows of 128 bytes, 16-byte pieces swizzled), written by all its lanes, on its way out.  A TMA
 // store ends at a multiple of 16 bytes, not at the matrix's last column: a box that the last column cuts elsewhere is
 // written by the lanes, so that nothing beyond column N changes.
@@ -450,12 +468,14 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 }
                 float top = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 128; ++i) {
-                    v[i] += bias[i];
-                    if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
-                    v[i] = col0 + i < p.N ? v[i] : 0.0f;
-                    top = fmaxf(top, fabsf(v[i]));
+                for (int j = 0; j < 4; ++j) add_bias_and_act<32>(v + 32 * j, bias + 32 * j, p.act);
+                if (col0 + 128 > p.N) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (col0 + i >= p.N) v[i] = 0.0f;
                 }
+#pragma unroll
+                for (int i = 0; i < 128; ++i) top = fmaxf(top, fabsf(v[i]));
                 if (__float_as_uint(top) == 0x7F800000u) {
                     top = 0.0f;
 #pragma unroll
@@ -496,10 +516,8 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                     }
                     float v[32];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        v[i] = __uint_as_float(r[i]) + bias[j * 32 + i];
-                        if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
-                    }
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+                    add_bias_and_act<32>(v, bias + j * 32, p.act);
                     constexpr int kBlocks = kCols / 32;       // blocks per box
                     if (jj % kBlocks == 0) {
                         if (lane == 0) tma_store_wait_read<0>();
