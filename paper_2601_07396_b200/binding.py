@@ -424,7 +424,11 @@ def svdcache_left_factors(C: torch.Tensor, sigma: torch.Tensor, stream=None) -> 
 
 ACT_NONE, ACT_GELU = 0, 1
 _BYTES = (torch.uint8, torch.float8_e4m3fn)
-_gemm_status = {}
+_SCALES = (torch.uint8, torch.float8_e8m0fnu)
+_gemm_status = {}   # device index -> the device's status word
+# The current stream's handle without building a torch.cuda.Stream around it (0.1 us instead of 3.4): these calls can
+# be shorter than that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
@@ -435,29 +439,47 @@ def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
 
 def _matrix(t: torch.Tensor, what: str):
     """(pointer, row pitch in elements) of a device matrix whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] != 1):
-        raise ValueError(f"{what}: a device matrix with contiguous rows is expected")
+    stride = t.stride()
+    if len(stride) != 2 or not t.is_cuda or stride[1] != 1:
+        if t.dim() != 2 or not t.is_cuda or t.shape[1] != 1:
+            raise ValueError(f"{what}: a device matrix with contiguous rows is expected")
     if t.shape[0] == 1:   # torch gives a single row any stride
         return t.data_ptr(), -(-t.shape[1] // 16) * 16
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _fp8_matrix(q: torch.Tensor, s: torch.Tensor, rows: int, cols: int, what: str):
-    if q.dtype not in _BYTES or q.shape[0] != rows or q.shape[1] < cols:
+    """(pointer of the bytes, pitch, pointer of the scales) of an 8-bit matrix."""
+    shape = q.shape
+    if shape[0] != rows or shape[1] < cols or q.dtype not in _BYTES:
         raise ValueError(f"{what}: {rows} x {cols} bytes are expected")
-    if not s.is_cuda or s.element_size() != 1 or not s.is_contiguous() or s.numel() < -(-rows // 128) * -(-cols // 512) * 512:
+    if s.nbytes < (rows + 127) // 128 * ((cols + 511) // 512) * 512 or s.dtype not in _SCALES or not s.is_cuda or not s.is_contiguous():
         raise ValueError(f"{what}: a scale buffer of svdcache_fp8_scale_bytes({rows}, {cols}) bytes is expected")
-    return _matrix(q, what)
+    return *_matrix(q, what), s.data_ptr()
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} fp32 values on the device are expected")
+    return t.data_ptr()
+
+
+def _stream_of(t: torch.Tensor, stream):
+    """The stream to launch on: the given one, or the current one of the tensor's device."""
+    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def svdcache_quantize_fp8(X: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, tile_rows: int = 1, stream=None) -> None:
     """X [rows, cols] fp32 or bf16 -> e4m3 bytes Q [rows, >= cols] and their scales S (see new_fp8); one scale per
     1 x 128 group, or with tile_rows = 128 per 128 x 128 tile."""
-    rows, cols = X.shape
     x, ld = _matrix(X, "X")
-    q, ldq = _fp8_matrix(Q, S, rows, cols, "Q")
-    _check(lib().svdcache_quantize_fp8(x, rows, cols, ld, _dt(X), tile_rows, q, ldq, S.data_ptr(), _stream(stream)),
-           "quantize_fp8")
+    rows, cols = X.shape
+    q, ldq, s = _fp8_matrix(Q, S, rows, cols, "Q")
+    rc = (_lib or lib()).svdcache_quantize_fp8(x, rows, cols, ld, _DTYPES[X.dtype], tile_rows, q, ldq, s, _stream_of(X, stream))
+    if rc:
+        raise SvdCacheError(rc, "quantize_fp8")
 
 
 def svdcache_residual_rmsnorm_fp8(H: torch.Tensor, X: Optional[torch.Tensor], H_out: Optional[torch.Tensor],
@@ -465,23 +487,24 @@ def svdcache_residual_rmsnorm_fp8(H: torch.Tensor, X: Optional[torch.Tensor], H_
                                   stream=None) -> None:
     """h = H + X (X None: h = H) -> H_out (None: not kept; H itself: in place); RMS norm of h times weight [D] fp32
     (None: ones) as an 8-bit matrix Q, S."""
-    rows, D = H.shape
     h, ldh = _matrix(H, "H")
-    x = ldx = o = ldo = w = None
-    for t, what in ((X, "X"), (H_out, "H_out")):
-        if t is not None and (t.shape != H.shape or t.dtype != H.dtype):
-            raise ValueError(f"{what}: H's shape and type are expected")
+    shape, dtype = H.shape, H.dtype
+    rows, D = shape
+    x = o = None
+    ldx = ldo = 0
     if X is not None:
+        if X.shape != shape or X.dtype != dtype:
+            raise ValueError("X: H's shape and type are expected")
         x, ldx = _matrix(X, "X")
     if H_out is not None:
+        if H_out.shape != shape or H_out.dtype != dtype:
+            raise ValueError("H_out: H's shape and type are expected")
         o, ldo = _matrix(H_out, "H_out")
-    if weight is not None:
-        if weight.dtype != torch.float32 or weight.shape != (D,) or not weight.is_cuda or not weight.is_contiguous():
-            raise ValueError("weight: D fp32 values on the device are expected")
-        w = weight.data_ptr()
-    q, ldq = _fp8_matrix(Q, S, rows, D, "Q")
-    _check(lib().svdcache_residual_rmsnorm_fp8(h, ldh, x, ldx or 0, o, ldo or 0, w, eps, q, ldq, S.data_ptr(), rows, D,
-                                               _dt(H), _stream(stream)), "residual_rmsnorm_fp8")
+    q, ldq, s = _fp8_matrix(Q, S, rows, D, "Q")
+    rc = (_lib or lib()).svdcache_residual_rmsnorm_fp8(h, ldh, x, ldx, o, ldo, _vector(weight, D, "weight"), eps, q, ldq, s, rows, D,
+                                                       _DTYPES[dtype], _stream_of(H, stream))
+    if rc:
+        raise SvdCacheError(rc, "residual_rmsnorm_fp8")
 
 
 def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: torch.Tensor, K: int, C: torch.Tensor,
@@ -491,38 +514,34 @@ def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: to
     (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
     one per device, which gemm_status() reads."""
     M, N = C.shape
-    a, lda = _fp8_matrix(A, SA, M, K, "A")
-    b, ldb = _fp8_matrix(B, SB, N, K, "B")
-    sc = bi = None
-    if C.dtype in _BYTES:
+    a, lda, sa = _fp8_matrix(A, SA, M, K, "A")
+    b, ldb, sb = _fp8_matrix(B, SB, N, K, "B")
+    dtype = C.dtype
+    if dtype in _BYTES:
         if S_out is None:
             raise ValueError("S_out: an 8-bit C needs a scale buffer")
-        out, sc = FP8, S_out.data_ptr()
-        c, ldc = _fp8_matrix(C, S_out, M, N, "C")
+        out = FP8
+        c, ldc, sc = _fp8_matrix(C, S_out, M, N, "C")
     else:
-        out = _dt(C)
+        out, sc = _DTYPES[dtype], None
         c, ldc = _matrix(C, "C")
-    if bias is not None:
-        if bias.dtype != torch.float32 or bias.shape != (N,) or not bias.is_cuda or not bias.is_contiguous():
-            raise ValueError("bias: N fp32 values on the device are expected")
-        bi = bias.data_ptr()
     if status is None:
-        status = _gemm_status.get(C.device)
+        status = _gemm_status.get(C.get_device())
         if status is None:
-            status = _gemm_status[C.device] = torch.zeros(1, dtype=torch.int32, device=C.device)
+            status = _gemm_status[C.get_device()] = torch.zeros(1, dtype=torch.int32, device=C.device)
             torch.cuda.synchronize(C.device)   # the zero is there whatever stream the product runs on
-    _check(lib().svdcache_gemm_fp8(a, lda, SA.data_ptr(), b, ldb, SB.data_ptr(), bi, act, c, ldc, out, sc, M, N, K,
-                                   status.data_ptr(), _stream(stream)), "gemm_fp8")
+    rc = (_lib or lib()).svdcache_gemm_fp8(a, lda, sa, b, ldb, sb, _vector(bias, N, "bias"), act, c, ldc, out, sc, M, N, K,
+                                           status.data_ptr(), _stream_of(C, stream))
+    if rc:
+        raise SvdCacheError(rc, "gemm_fp8")
 
 
 def gemm_status(device="cuda") -> int:
     """The sticky status of the products on `device` that were given no status word (synchronises): 0, or -6 if a
     bounded wait ran out in one of them."""
     device = torch.device(device)
-    if device.index is None:
-        device = torch.device(device.type, torch.cuda.current_device())
     torch.cuda.synchronize(device)
-    status = _gemm_status.get(device)
+    status = _gemm_status.get(torch.cuda.current_device() if device.index is None else device.index)
     return 0 if status is None else int(status.item())
 
 

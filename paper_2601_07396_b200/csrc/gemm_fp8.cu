@@ -11,6 +11,7 @@
 // tile, each sums its own K range, and after one cluster barrier each adds up its share of the rows over the
 // cluster in rank order (distributed shared memory): no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
+#include <atomic>
 #include <type_traits>
 
 #include "fp8.cuh"
@@ -68,6 +69,70 @@ __device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int 
         } else {
             for (int i = 0; i < 4; ++i)
                 if (n + i < p.N) o[i] = __float2bfloat16_rn(v[i]);
+        }
+    }
+}
+
+// The rows of a tile are dealt to its cluster's S CTAs in equal runs, and within a CTA to the warps, R at a time, four
+// columns per lane: the sum over the cluster in rank order, bias, activation, and out.  R * S loads are in flight.
+template <int S, int R>
+__device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t base, int rank, int64_t m0, int n_tile) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per = (p.tile_m + S - 1) / S, r_lo = rank * per;
+    const int r_hi = min(min(r_lo + per, p.tile_m), (int)(p.M - m0 < p.tile_m ? p.M - m0 : p.tile_m));
+    const int n = n_tile * kTileN + 4 * lane;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (p.bias)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.N) bias[i] = p.bias[n + i];
+    for (int r0 = r_lo + warp * R; r0 < r_hi; r0 += kTileThreads / 32 * R) {
+        float4 part[R][S];
+#pragma unroll
+        for (int x = 0; x < S; ++x) {
+            const uint32_t from = S == 1 ? base : cluster_addr(base, (uint32_t)x);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const uint32_t at = from + (uint32_t)(min(r0 + i, p.tile_m - 1) * kTileN + 4 * lane) * 4u;
+                part[i][x] = S == 1 ? shared_load(at) : cluster_load(at);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            float v[4] = {part[i][0].x, part[i][0].y, part[i][0].z, part[i][0].w};
+#pragma unroll
+            for (int x = 1; x < S; ++x) {
+                v[0] += part[i][x].x; v[1] += part[i][x].y; v[2] += part[i][x].z; v[3] += part[i][x].w;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] += bias[j];
+                if (p.act == SVDCACHE_ACT_GELU) v[j] = gelu_tanh(v[j]);
+            }
+            const int64_t m = m0 + r0 + i;
+            const bool live = r0 + i < r_hi;
+            if (p.out != SVDCACHE_FP8) {
+                if (live) store_plain(p, m, n, v);
+                continue;
+            }
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = n + j < p.N ? fp8_nan_if_not_finite(v[j]) : 0.0f;
+                top = fmaxf(top, fabsf(v[j]));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const uint32_t byte = fp8_scale_byte(top);
+            const float inv = fp8_inverse_scale(byte);
+            const uint32_t w = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            if (!live) continue;
+            uint8_t *o = reinterpret_cast<uint8_t *>(p.C) + m * p.ldc + n;
+            if (n + 4 <= p.N) *reinterpret_cast<uint32_t *>(o) = w;
+            else
+                for (int j = 0; j < 4; ++j)
+                    if (n + j < p.N) o[j] = (uint8_t)(w >> (8 * j));
+            if (lane == 0) p.SC[fp8_scale_offset(m, n_tile, p.pieces_c)] = (uint8_t)byte;
         }
     }
 }
@@ -197,49 +262,11 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     }
     if (p.splits > 1) cluster_sync();
 
-    // rows of the tile are dealt to the cluster's CTAs in equal runs, a warp per row, four columns per lane
-    const int per = (p.tile_m + p.splits - 1) / p.splits, r_lo = rank * per;
-    const int r_hi = min(min(r_lo + per, p.tile_m), (int)(p.M - m0 < p.tile_m ? p.M - m0 : p.tile_m));
-    const int n = n0 + 4 * lane;
-    float bias[4] = {0.f, 0.f, 0.f, 0.f};
-    if (p.bias)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < p.N) bias[i] = p.bias[n + i];
-    for (int r = r_lo + warp; r < r_hi; r += kTileThreads / 32) {
-        const uint32_t at = base + (uint32_t)(r * kTileN + 4 * lane) * 4u;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int x = 0; x < p.splits; ++x) {
-            const float4 w = cluster_load(cluster_addr(at, (uint32_t)x));
-            v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] += bias[i];
-            if (p.act == SVDCACHE_ACT_GELU) v[i] = gelu_tanh(v[i]);
-        }
-        const int64_t m = m0 + r;
-        if (p.out != SVDCACHE_FP8) {
-            store_plain(p, m, n, v);
-            continue;
-        }
-        float top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = n + i < p.N ? fp8_nan_if_not_finite(v[i]) : 0.0f;
-            top = fmaxf(top, fabsf(v[i]));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const uint32_t byte = fp8_scale_byte(top);
-        const float inv = fp8_inverse_scale(byte);
-        const uint32_t w = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-        uint8_t *o = reinterpret_cast<uint8_t *>(p.C) + m * p.ldc + n;
-        if (n + 4 <= p.N) *reinterpret_cast<uint32_t *>(o) = w;
-        else
-            for (int i = 0; i < 4; ++i)
-                if (n + i < p.N) o[i] = (uint8_t)(w >> (8 * i));
-        if (lane == 0) p.SC[fp8_scale_offset(m, n_tile, p.pieces_c)] = (uint8_t)byte;
+    switch (p.splits) {
+        case 1: finish_rows<1, 4>(p, base, rank, m0, n_tile); break;
+        case 2: finish_rows<2, 4>(p, base, rank, m0, n_tile); break;
+        case 4: finish_rows<4, 4>(p, base, rank, m0, n_tile); break;
+        default: finish_rows<8, 2>(p, base, rank, m0, n_tile); break;
     }
     if (p.splits > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
 }
@@ -263,6 +290,7 @@ constexpr uint32_t kPairScaleBytes = 3 * kScalePieceBytes;                      
 constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes + 2048;
 constexpr uint32_t kStoreBytes = 32 * 128;                                        // a warp's box of C: 32 rows of 128 bytes
 constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStageBytes + 8 * kStoreBytes;
+static_assert(kPairSmem <= 222 * 1024, "dynamic shared memory");
 constexpr uint32_t kAccStep = 224, kScaleCol = 480;
 constexpr int kRasterRows = 8;      // tile rows that neighbouring clusters share: 8 x n tiles are walked column by column
 
@@ -604,16 +632,26 @@ int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t l
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
-int sm_count() {
-    int dev = 0, n = 0;
-    cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    return n > 0 ? n : 148;
+// What the launches ask of the current device, asked once per device: its SMs, and leave for its kernels to
+// use more dynamic shared memory than the default (up to kSmemLimit).
+constexpr int kSmemLimit = 227 * 1024 - 5 * 1024;    // the static part of any of the kernels is below 5 KB
+constexpr int kMaxDevices = 64;
+
+int device_ready(int *sms) {
+    static std::atomic<int> known[kMaxDevices];
+    int dev = 0;
+    int rc = record_cuda(cudaGetDevice(&dev));
+    if (rc) return rc;
+    if (dev < kMaxDevices && (*sms = known[dev].load(std::memory_order_acquire)) > 0) return SVDCACHE_OK;
+    rc = record_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    for (const void *k : {(const void *)tile_kernel, (const void *)pair_kernel<SVDCACHE_F32>, (const void *)pair_kernel<SVDCACHE_BF16>,
+                          (const void *)pair_kernel<SVDCACHE_FP8>})
+        if (!rc) rc = record_cuda(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+    if (!rc && dev < kMaxDevices) known[dev].store(*sms, std::memory_order_release);
+    return rc;
 }
 
-constexpr size_t kSmemBudget = 225 * 1024;   // of 227 KB: the barriers are static
-
-int tile_launch(const GemmFp8Args &a, cudaStream_t s) {
+int tile_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     TileParams p{};
     p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
@@ -623,12 +661,12 @@ int tile_launch(const GemmFp8Args &a, cudaStream_t s) {
     p.n_tiles = (a.N + kTileN - 1) / kTileN;
     const int64_t tiles = (a.M + p.tile_m - 1) / p.tile_m * p.n_tiles;
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= sm_count() && p.groups >= 2 * p.splits) p.splits *= 2;
+    while (p.splits < 8 && tiles * p.splits * 2 <= sms && p.groups >= 2 * p.splits) p.splits *= 2;
     if (tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + (p.a_bytes < 1024 * 32 ? 1024u : 2048u);
     p.tmem_cols = p.tile_m <= 32 ? 64 : p.tile_m == 64 ? 128 : p.tile_m == 128 ? 256 : 512;
-    int stages = (int)((kSmemBudget - 1024) / p.stage_bytes);
+    int stages = (kSmemLimit - 1024) / (int)p.stage_bytes;
     if (stages > kMaxStages) stages = kMaxStages;
     const int longest = (p.groups + p.splits - 1) / p.splits;
     const int least = (int)(((size_t)p.tile_m * kTileN * 4 + p.stage_bytes - 1) / p.stage_bytes);   // the accumulator passes through the ring
@@ -639,7 +677,6 @@ int tile_launch(const GemmFp8Args &a, cudaStream_t s) {
     CUtensorMap tm_a, tm_b;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
     if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, kTileN);
-    if (!rc) rc = record_cuda(cudaFuncSetAttribute(tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (rc) return rc;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(tiles * p.splits));
@@ -689,7 +726,7 @@ int out_map(CUtensorMap *m, const GemmFp8Args &a) {
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
-int pair_launch(const GemmFp8Args &a, cudaStream_t s) {
+int pair_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     PairParams p{};
     p.M = a.M; p.N = a.N; p.groups = (int)fp8_groups(a.K); p.C = a.C; p.ldc = a.ldc;
     p.n_tiles = (a.N + kPairN - 1) / kPairN;
@@ -705,10 +742,8 @@ int pair_launch(const GemmFp8Args &a, cudaStream_t s) {
     if (!rc) rc = scale_map(&tm_sb, a.SB, a.N, fp8_piece_cols(a.K));
     if (!rc) rc = out_map(&tm_c, a);
     if (rc) return rc;
-    const int clusters = sm_count() / 2 < p.tiles ? sm_count() / 2 : p.tiles;
+    const int clusters = sms / 2 < p.tiles ? sms / 2 : p.tiles;
     auto launch = [&](auto kern) {
-        const int e = record_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairSmem));
-        if (e) return e;
         kern<<<2 * clusters, kPairThreads, kPairSmem, s>>>(tm_a, tm_b, tm_sa, tm_sb, tm_c, p);
         count_launch();
         return check_last_launch();
@@ -720,8 +755,11 @@ int pair_launch(const GemmFp8Args &a, cudaStream_t s) {
 }  // namespace
 
 int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
-    if (a.M > 256 && a.N > 256) return pair_launch(a, s);
-    return tile_launch(a, s);
+    int sms = 0;
+    const int rc = device_ready(&sms);
+    if (rc) return rc;
+    if (a.M > 256 && a.N > 256) return pair_launch(a, sms, s);
+    return tile_launch(a, sms, s);
 }
 
 }  // namespace svdc

@@ -1,11 +1,14 @@
 // Eight-bit outputs of elementwise and row-wise work (format: fp8.cuh):
-//   quantize_rows_kernel    a matrix as e4m3 with a scale per 1 x 128 group (activations)
-//   quantize_tiles_kernel   the same with one scale per 128 x 128 tile, repeated for its rows (weights)
-//   rmsnorm_kernel          h' = h + x;  y = h' * rsqrt(mean(h'^2) + eps) * w;  y as e4m3 with a scale per group
-// All three read every input once and write every output once: bandwidth-bound.  The common step is a chunk of
+//   rows_kernel<.., false>   a matrix as e4m3 with a scale per 1 x 128 group (activations)
+//   rows_kernel<.., true>    h' = h + x;  y = h' * rsqrt(mean(h'^2) + eps) * w;  y as e4m3 with a scale per group
+//   tiles_kernel             a matrix with one scale per 128 x 128 tile, repeated for its rows (weights)
+// All of it reads every input once and writes every output once: bandwidth-bound.  The common step is a chunk of
 // eight elements per thread, so that 16 neighbouring lanes hold one group and its maximum takes four shuffles.
 // Arithmetic is fp32 throughout; h' is rounded to the I/O type only where it is stored, and y is formed from
 // the unrounded h'.
+#include <cstring>
+#include <type_traits>
+
 #include "fp8.cuh"
 
 namespace svdc {
@@ -14,6 +17,7 @@ namespace {
 constexpr int kChunk = 8;                           // elements per thread and step: 16 bytes of bf16, 32 of fp32
 constexpr int kGroupLanes = kFp8Group / kChunk;     // 16 lanes hold a group
 constexpr int kThreads = 256;
+constexpr int kMaxCta = 512;                        // 16 warps of four chunks per lane: a row of 16384
 
 template <bool BF16> struct Raw;                    // a chunk as it lies in memory
 template <> struct Raw<true> { uint4 a; };
@@ -55,29 +59,28 @@ template <bool BF16> __device__ __forceinline__ void store_chunk(void *row, int 
     }
 }
 
-// chunk c0 of a row `cols` long, zeros beyond its end; a chunk that the end cuts is read element by element
-template <bool BF16> __device__ __forceinline__ void load_cut_chunk(const void *row, int c0, int cols, float (&v)[kChunk]) {
-    if (c0 + kChunk <= cols) {
-        to_float<BF16>(load_chunk<BF16>(row, c0), v);
-        return;
-    }
+// Chunk c0 of a row `cols` long, zeros beyond its end and where `live` is false.  CUT: cols is not a multiple of 8,
+// so that the end may cut a chunk, which is then read element by element.
+template <bool BF16, bool CUT>
+__device__ __forceinline__ Raw<BF16> load_live_chunk(const void *row, int c0, int cols, bool live) {
+    Raw<BF16> r{};
+    if (live && c0 + (CUT ? kChunk : 1) <= cols) r = load_chunk<BF16>(row, c0);
+    else if (CUT && live) {
+        using T = typename std::conditional<BF16, __nv_bfloat16, float>::type;
+        T e[kChunk];
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) {
-        v[i] = 0.0f;
-        if (c0 + i < cols) {
-            if constexpr (BF16) v[i] = __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(row)[c0 + i]);
-            else v[i] = reinterpret_cast<const float *>(row)[c0 + i];
-        }
+        for (int i = 0; i < kChunk; ++i) e[i] = c0 + i < cols ? reinterpret_cast<const T *>(row)[c0 + i] : T(0.0f);
+        memcpy(&r, e, sizeof(r));
     }
+    return r;
 }
-__device__ __forceinline__ void store_cut_bytes(uint8_t *row, int c0, int cols, uint2 w) {
-    if (c0 + kChunk <= cols) {
-        *reinterpret_cast<uint2 *>(row + c0) = w;
-        return;
-    }
+template <bool CUT> __device__ __forceinline__ void store_live_bytes(uint8_t *row, int c0, int cols, uint2 w) {
+    if (c0 + (CUT ? kChunk : 1) <= cols) *reinterpret_cast<uint2 *>(row + c0) = w;
+    else if (CUT) {
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i)
-        if (c0 + i < cols) row[c0 + i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+        for (int i = 0; i < kChunk; ++i)
+            if (c0 + i < cols) row[c0 + i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
 }
 
 __device__ __forceinline__ float largest(const float (&v)[kChunk]) {   // NaN is passed over, Inf is not
@@ -93,15 +96,9 @@ __device__ __forceinline__ float group_max(float m) {
     return m;
 }
 __device__ __forceinline__ bool is_inf(float m) { return __float_as_uint(m) == 0x7F800000u; }
-// the maximum over the group's finite values; elements that are Inf become NaN.  Called by whole warps.
-__device__ __forceinline__ float finite_group_max(float (&v)[kChunk]) {
-    float m = group_max(largest(v));
-    if (__any_sync(0xFFFFFFFFu, is_inf(m))) {
+__device__ __forceinline__ void drop_infinities(float (&v)[kChunk]) {   // they become NaN, which the format has
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = fp8_nan_if_not_finite(v[i]);
-        m = group_max(largest(v));
-    }
-    return m;
+    for (int i = 0; i < kChunk; ++i) v[i] = fp8_nan_if_not_finite(v[i]);
 }
 __device__ __forceinline__ uint2 scaled_bytes(const float (&v)[kChunk], uint32_t byte) {
     const float inv = fp8_inverse_scale(byte);
@@ -111,59 +108,160 @@ __device__ __forceinline__ uint2 scaled_bytes(const float (&v)[kChunk], uint32_t
     return w;
 }
 
-// ------------------------------------------------------------------------------------------ quantiser ---
+// ----------------------------------------------------------------------------------------------- rows ---
 
-struct QuantArgs {
-    const void *X;
+struct RowsArgs {
+    const void *H, *X;      // NORM: X null: no addition
+    void *H_out;            // NORM: null: h' is not stored
+    const float *weight;    // NORM: null: ones
     uint8_t *Q, *S;
-    int64_t rows, ld, ldq;
-    int cols, groups, rows_per_cta;
+    int64_t ldh, ldx, ldo, ldq, rows;
+    int cols, warps;        // warps per row
+    float eps;
     int64_t pieces;
 };
 
-// A CTA takes rows_per_cta rows; 16 lanes take a group at a time.
-template <bool BF16> __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const QuantArgs a) {
-    const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_cta;
-    const int nrows = (int)(a.rows - row0 < a.rows_per_cta ? a.rows - row0 : a.rows_per_cta);
-    const int units = nrows * a.groups, lane = threadIdx.x % kGroupLanes;
-    constexpr int kAtOnce = kThreads / kGroupLanes;
-    for (int u0 = 0; u0 < units; u0 += kAtOnce) {   // the same number of steps for every lane of a warp
-        const int u = u0 + (int)threadIdx.x / kGroupLanes;
-        const bool live = u < units;
-        const int r = live ? u / a.groups : 0, g = live ? u - r * a.groups : 0;
-        const int64_t m = row0 + r;
-        const int c0 = g * kFp8Group + lane * kChunk;
-        float v[kChunk] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live)
-            load_cut_chunk<BF16>(reinterpret_cast<const char *>(a.X) + (size_t)m * a.ld * (BF16 ? 2 : 4), c0, a.cols, v);
-        const uint32_t byte = fp8_scale_byte(finite_group_max(v));
-        if (live) {
-            store_cut_bytes(a.Q + (size_t)m * a.ldq, c0, a.cols, scaled_bytes(v, byte));
-            if (lane == 0) a.S[fp8_scale_offset(m, g, a.pieces)] = (uint8_t)byte;
+// A row (NORM) or a segment of one (blockIdx.y) belongs to a.warps warps, V chunks per lane, consecutive runs of 32
+// chunks per warp and step: 128 bytes of bf16 in flight per lane and input at V = 4.  Values stay in fp32 registers
+// from the load to the rounding.
+template <bool BF16, bool CUT, bool NORM, int V> __global__ void __launch_bounds__(kMaxCta) rows_kernel(const RowsArgs a) {
+    __shared__ float part[kMaxCta / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int in_cta = warp / a.warps, at = warp - in_cta * a.warps;        // row of the CTA, warp of the row
+    const int64_t m = (int64_t)blockIdx.x * (blockDim.x / 32 / a.warps) + in_cta;
+    const bool live = m < a.rows;
+    const int step0 = (blockIdx.y * a.warps + at) * V, first = (step0 * 32 + lane) * kChunk;   // this lane's columns: first + 256 j
+    constexpr int e = BF16 ? 2 : 4;
+    float v[V][kChunk];
+    {
+        Raw<BF16> rh[V], rx[NORM ? V : 1];
+        const char *h_row = reinterpret_cast<const char *>(a.H) + (size_t)m * a.ldh * e;
+#pragma unroll
+        for (int j = 0; j < V; ++j) rh[j] = load_live_chunk<BF16, CUT>(h_row, first + 256 * j, a.cols, live);
+        if (NORM && a.X) {
+            const char *x_row = reinterpret_cast<const char *>(a.X) + (size_t)m * a.ldx * e;
+#pragma unroll
+            for (int j = 0; j < V; ++j) rx[NORM ? j : 0] = load_live_chunk<BF16, CUT>(x_row, first + 256 * j, a.cols, live);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            to_float<BF16>(rh[j], v[j]);
+            if (NORM && a.X) {
+                float x[kChunk];
+                to_float<BF16>(rx[NORM ? j : 0], x);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) v[j][i] += x[i];
+            }
+        }
+    }
+    if constexpr (NORM) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) sum = fmaf(v[j][i], v[j][i], sum);
+            if (a.H_out && live && first + 256 * j < a.cols)
+                store_chunk<BF16>(reinterpret_cast<char *>(a.H_out) + (size_t)m * a.ldo * e, first + 256 * j, v[j]);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (a.warps > 1) {
+            if (lane == 0) part[warp] = sum;
+            __syncthreads();
+            sum = 0.0f;
+            for (int w = 0; w < a.warps; ++w) sum += part[in_cta * a.warps + w];
+        }
+        const float inv_rms = rsqrtf(sum / (float)a.cols + a.eps);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const bool in = first + 256 * j < a.cols;
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) v[j][i] = in ? v[j][i] * inv_rms : 0.0f;   // 0 * inv_rms is not 0 in every row
+            if (a.weight && in) {
+                const float4 w0 = *reinterpret_cast<const float4 *>(a.weight + first + 256 * j);
+                const float4 w1 = *reinterpret_cast<const float4 *>(a.weight + first + 256 * j + 4);
+                v[j][0] *= w0.x; v[j][1] *= w0.y; v[j][2] *= w0.z; v[j][3] *= w0.w;
+                v[j][4] *= w1.x; v[j][5] *= w1.y; v[j][6] *= w1.z; v[j][7] *= w1.w;
+            }
+        }
+    }
+    float top[V], most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        top[j] = group_max(largest(v[j]));
+        most = fmaxf(most, top[j]);
+    }
+    if (__any_sync(0xFFFFFFFFu, is_inf(most))) {   // a group's scale is that of its finite values
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            drop_infinities(v[j]);
+            top[j] = group_max(largest(v[j]));
+        }
+    }
+    uint8_t *q_row = a.Q + (size_t)m * a.ldq;
+    uint8_t *s_row = a.S + fp8_scale_offset(m, 0, a.pieces);
+    uint32_t byte[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        byte[j] = fp8_scale_byte(top[j]);
+        if (live) store_live_bytes<CUT>(q_row, first + 256 * j, a.cols, scaled_bytes(v[j], byte[j]));
+    }
+    // group 2 (step0 + j) + lane / 16.  Two steps from an even one on make a whole word of four scales, unless the
+    // row ends inside it.
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int g = 2 * (step0 + j), off = g / kScaleGroups * kScalePieceBytes + (g & 3);
+        if (V % 2 == 0 && (j & 1) == 0 && (g + 3) * kFp8Group < a.cols) {
+            const uint32_t both = byte[j] | byte[(j + 1) % V] << 16, other = __shfl_xor_sync(0xFFFFFFFFu, both, 16);
+            if (live && lane == 0) *reinterpret_cast<uint32_t *>(s_row + off) = both | other << 8;
+            ++j;
+        } else if (live && lane % kGroupLanes == 0 && first + 256 * j < a.cols) {
+            s_row[off + lane / kGroupLanes] = (uint8_t)byte[j];
         }
     }
 }
 
-// One CTA per 128 x 128 tile, held in registers between the maximum and the rounding.
-template <bool BF16> __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(const QuantArgs a) {
+// ---------------------------------------------------------------------------------------------- tiles ---
+
+struct TilesArgs {
+    const void *X;
+    uint8_t *Q, *S;
+    int64_t rows, ld, ldq;
+    int cols, groups;
+    int64_t pieces;
+};
+
+// One CTA per 128 x 128 tile, held in registers as it was read between the maximum and the rounding.
+template <bool BF16, bool CUT> __global__ void __launch_bounds__(kThreads) tiles_kernel(const TilesArgs a) {
     constexpr int kRowsAtOnce = kThreads / kGroupLanes, kSteps = kScaleRows / kRowsAtOnce;   // 16 rows, 8 steps
     __shared__ float part[kThreads / 32];
     const int64_t row0 = (int64_t)(blockIdx.x / a.groups) * kScaleRows;
     const int g = (int)(blockIdx.x % a.groups), lane = threadIdx.x % kGroupLanes;
     const int c0 = g * kFp8Group + lane * kChunk;
-    float v[kSteps][kChunk];
-    float top = 0.0f;
+    Raw<BF16> raw[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int64_t m = row0 + i * kRowsAtOnce + threadIdx.x / kGroupLanes;
+        raw[i] = load_live_chunk<BF16, CUT>(reinterpret_cast<const char *>(a.X) + (size_t)m * a.ld * (BF16 ? 2 : 4), c0, a.cols, m < a.rows);
+    }
+    float v[kChunk], top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) v[i][j] = 0.0f;
-        if (m < a.rows)
-            load_cut_chunk<BF16>(reinterpret_cast<const char *>(a.X) + (size_t)m * a.ld * (BF16 ? 2 : 4), c0, a.cols, v[i]);
+    for (int i = 0; i < kSteps; ++i) {
+        to_float<BF16>(raw[i], v);
+        top = fmaxf(top, largest(v));
+    }
+    const bool inf = __syncthreads_or(is_inf(top));   // an Inf anywhere in the tile: the maximum over what is finite
+    if (inf) {
+        top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            to_float<BF16>(raw[i], v);
+            drop_infinities(v);
+            top = fmaxf(top, largest(v));
+        }
     }
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) top = fmaxf(top, finite_group_max(v[i]));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, kGroupLanes));
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
     __syncthreads();
 #pragma unroll
@@ -172,161 +270,68 @@ template <bool BF16> __global__ void __launch_bounds__(kThreads) quantize_tiles_
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int64_t m = row0 + i * kRowsAtOnce + threadIdx.x / kGroupLanes;
-        if (m < a.rows) store_cut_bytes(a.Q + (size_t)m * a.ldq, c0, a.cols, scaled_bytes(v[i], byte));
+        to_float<BF16>(raw[i], v);
+        if (inf) drop_infinities(v);
+        if (m < a.rows) store_live_bytes<CUT>(a.Q + (size_t)m * a.ldq, c0, a.cols, scaled_bytes(v, byte));
     }
     if (threadIdx.x < kScaleRows && row0 + threadIdx.x < a.rows)
         a.S[fp8_scale_offset(row0 + threadIdx.x, g, a.pieces)] = (uint8_t)byte;
 }
 
-// ------------------------------------------------------------------- residual addition and RMS norm ---
-
-struct NormArgs {
-    const void *H, *X;      // X null: no addition
-    void *H_out;            // null: h' is not stored
-    const float *weight;    // null: ones
-    uint8_t *Q, *S;
-    int64_t ldh, ldx, ldo, ldq, rows;
-    int D;
-    float eps;
-    int64_t pieces;
-};
-
-// TPR threads per row, V chunks of 8 elements per thread, held in fp32 registers from the load to the rounding.
-template <bool BF16, int TPR, int V> __global__ void __launch_bounds__(TPR > kThreads ? TPR : kThreads) rmsnorm_kernel(const NormArgs a) {
-    constexpr int kCta = TPR > kThreads ? TPR : kThreads, kRows = kCta / TPR, kWarps = TPR / 32;
-    __shared__ float part[kCta / 32];
-    const int64_t m = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    const int t = threadIdx.x % TPR;
-    const bool live = m < a.rows;
-    constexpr int e = BF16 ? 2 : 4;
-    const char *h_row = reinterpret_cast<const char *>(a.H) + (size_t)m * a.ldh * e;
-    const char *x_row = reinterpret_cast<const char *>(a.X) + (size_t)m * a.ldx * e;
-    float v[V][kChunk];
-    float sum = 0.0f;
-    {
-        Raw<BF16> rh[V], rx[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = (j * TPR + t) * kChunk;
-            if (live && c0 < a.D) {
-                rh[j] = load_chunk<BF16>(h_row, c0);
-                if (a.X) rx[j] = load_chunk<BF16>(x_row, c0);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = (j * TPR + t) * kChunk;
-            const bool in = live && c0 < a.D;
-            float x[kChunk];
-            if (in) to_float<BF16>(rh[j], v[j]);
-            if (in && a.X) {
-                to_float<BF16>(rx[j], x);
-#pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[j][i] += x[i];
-            }
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) {
-                if (!in) v[j][i] = 0.0f;
-                sum = fmaf(v[j][i], v[j][i], sum);
-            }
-            if (in && a.H_out) store_chunk<BF16>(reinterpret_cast<char *>(a.H_out) + (size_t)m * a.ldo * e, c0, v[j]);
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    if constexpr (kWarps > 1) {
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
-        __syncthreads();
-        const int w0 = threadIdx.x / TPR * kWarps;
-        sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum += part[w0 + w];
-    }
-    const float inv_rms = rsqrtf(sum / (float)a.D + a.eps);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c0 = (j * TPR + t) * kChunk;
-        const bool in = live && c0 < a.D;
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[j][i] *= inv_rms;
-        if (in && a.weight) {
-            const float4 w0 = *reinterpret_cast<const float4 *>(a.weight + c0), w1 = *reinterpret_cast<const float4 *>(a.weight + c0 + 4);
-            v[j][0] *= w0.x; v[j][1] *= w0.y; v[j][2] *= w0.z; v[j][3] *= w0.w;
-            v[j][4] *= w1.x; v[j][5] *= w1.y; v[j][6] *= w1.z; v[j][7] *= w1.w;
-        }
-        if (!in) {   // lanes beyond the row hold 0 * inv_rms, which is not 0 in a row that is not finite
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) v[j][i] = 0.0f;
-        }
-        const uint32_t byte = fp8_scale_byte(finite_group_max(v[j]));
-        if (in) {
-            *reinterpret_cast<uint2 *>(a.Q + (size_t)m * a.ldq + c0) = scaled_bytes(v[j], byte);
-            if (t % kGroupLanes == 0) a.S[fp8_scale_offset(m, c0 / kFp8Group, a.pieces)] = (uint8_t)byte;
-        }
-    }
-}
-
-template <bool BF16, int TPR> int norm_launch_v(const NormArgs &a, int v, cudaStream_t s) {
-    constexpr int kCta = TPR > kThreads ? TPR : kThreads;
-    const int64_t grid = (a.rows + kCta / TPR - 1) / (kCta / TPR);
-    if (grid > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+// Lanes hold four chunks (8 KB of values per warp and input: the loads that hide the memory's latency at eight warps a
+// row of the CTA); fewer where the row is short.  Rows longer than `most` warps are cut into segments, which a norm
+// cannot be.
+template <bool BF16, bool CUT, bool NORM> int rows_launch(RowsArgs a, int most, cudaStream_t s) {
+    constexpr int kSteps = 4;
+    const int steps = (a.cols + 255) / 256, segments = (steps + most * kSteps - 1) / (most * kSteps);
+    const int per = (steps + segments - 1) / segments;               // steps of a segment
+    a.warps = (per + kSteps - 1) / kSteps;
+    const int v = (per + a.warps - 1) / a.warps;
+    const int rows_at_once = a.warps < kThreads / 32 ? kThreads / 32 / a.warps : 1;
+    const int64_t grid = (a.rows + rows_at_once - 1) / rows_at_once;
+    const dim3 blocks((unsigned)grid, (unsigned)((steps + a.warps * v - 1) / (a.warps * v))), threads(32 * a.warps * rows_at_once);
     switch (v) {
-        case 1: rmsnorm_kernel<BF16, TPR, 1><<<(unsigned)grid, kCta, 0, s>>>(a); break;
-        case 2: rmsnorm_kernel<BF16, TPR, 2><<<(unsigned)grid, kCta, 0, s>>>(a); break;
-        case 3: rmsnorm_kernel<BF16, TPR, 3><<<(unsigned)grid, kCta, 0, s>>>(a); break;
-        default: rmsnorm_kernel<BF16, TPR, 4><<<(unsigned)grid, kCta, 0, s>>>(a); break;
+        case 1: rows_kernel<BF16, CUT, NORM, 1><<<blocks, threads, 0, s>>>(a); break;
+        case 2: rows_kernel<BF16, CUT, NORM, 2><<<blocks, threads, 0, s>>>(a); break;
+        case 3: rows_kernel<BF16, CUT, NORM, 3><<<blocks, threads, 0, s>>>(a); break;
+        default: rows_kernel<BF16, CUT, NORM, 4><<<blocks, threads, 0, s>>>(a); break;
     }
     count_launch();
     return check_last_launch();
 }
 
-// The fewest threads per row (a power of two of warps) that hold a row in four chunks each.
-template <bool BF16> int norm_launch(const NormArgs &a, cudaStream_t s) {
-    const int chunks = a.D / kChunk;
-    int tpr = 32;
-    while ((chunks + tpr - 1) / tpr > 4) tpr *= 2;
-    const int v = (chunks + tpr - 1) / tpr;
-    switch (tpr) {
-        case 32: return norm_launch_v<BF16, 32>(a, v, s);
-        case 64: return norm_launch_v<BF16, 64>(a, v, s);
-        case 128: return norm_launch_v<BF16, 128>(a, v, s);
-        case 256: return norm_launch_v<BF16, 256>(a, v, s);
-        default: return norm_launch_v<BF16, 512>(a, v, s);
-    }
+template <bool BF16> int tiles_launch(const TilesArgs &a, cudaStream_t s) {
+    const int64_t grid = (a.rows + kScaleRows - 1) / kScaleRows * a.groups;
+    if (grid > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    if (a.cols % kChunk) tiles_kernel<BF16, true><<<(unsigned)grid, kThreads, 0, s>>>(a);
+    else tiles_kernel<BF16, false><<<(unsigned)grid, kThreads, 0, s>>>(a);
+    count_launch();
+    return check_last_launch();
 }
 
 }  // namespace
 
 int quantize_fp8_launch(const void *X, int64_t rows, int cols, int64_t ld, int dtype, int tile_rows, void *Q, int64_t ldq,
                         void *S, cudaStream_t s) {
-    QuantArgs a{};
-    a.X = X; a.Q = (uint8_t *)Q; a.S = (uint8_t *)S; a.rows = rows; a.ld = ld; a.ldq = ldq; a.cols = cols;
-    a.groups = (int)fp8_groups(cols); a.pieces = fp8_piece_cols(cols);
     const bool bf = dtype == SVDCACHE_BF16;
-    if (tile_rows == 1) {
-        // about four steps per CTA, so that each warp has several loads to wait for
-        constexpr int kUnits = 4 * kThreads / kGroupLanes;
-        a.rows_per_cta = a.groups >= kUnits ? 1 : kUnits / a.groups;
-        const int64_t grid = (rows + a.rows_per_cta - 1) / a.rows_per_cta;
-        if (grid > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-        if (bf) quantize_rows_kernel<true><<<(unsigned)grid, kThreads, 0, s>>>(a);
-        else quantize_rows_kernel<false><<<(unsigned)grid, kThreads, 0, s>>>(a);
-    } else {
-        const int64_t grid = (rows + kScaleRows - 1) / kScaleRows * a.groups;
-        if (grid > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-        if (bf) quantize_tiles_kernel<true><<<(unsigned)grid, kThreads, 0, s>>>(a);
-        else quantize_tiles_kernel<false><<<(unsigned)grid, kThreads, 0, s>>>(a);
+    if (tile_rows != 1) {
+        TilesArgs a{};
+        a.X = X; a.Q = (uint8_t *)Q; a.S = (uint8_t *)S; a.rows = rows; a.ld = ld; a.ldq = ldq; a.cols = cols;
+        a.groups = (int)fp8_groups(cols); a.pieces = fp8_piece_cols(cols);
+        return bf ? tiles_launch<true>(a, s) : tiles_launch<false>(a, s);
     }
-    count_launch();
-    return check_last_launch();
+    RowsArgs a{};
+    a.H = X; a.Q = (uint8_t *)Q; a.S = (uint8_t *)S; a.rows = rows; a.ldh = ld; a.ldq = ldq; a.cols = cols; a.pieces = fp8_piece_cols(cols);
+    if (cols % kChunk) return bf ? rows_launch<true, true, false>(a, 1, s) : rows_launch<false, true, false>(a, 1, s);
+    return bf ? rows_launch<true, false, false>(a, 1, s) : rows_launch<false, false, false>(a, 1, s);
 }
 
 int rmsnorm_fp8_launch(const void *H, int64_t ldh, const void *X, int64_t ldx, void *H_out, int64_t ldo, const float *weight,
                        float eps, void *Q, int64_t ldq, void *S, int64_t rows, int D, int dtype, cudaStream_t s) {
-    NormArgs a{};
+    RowsArgs a{};
     a.H = H; a.X = X; a.H_out = H_out; a.weight = weight; a.Q = (uint8_t *)Q; a.S = (uint8_t *)S;
-    a.ldh = ldh; a.ldx = ldx; a.ldo = ldo; a.ldq = ldq; a.rows = rows; a.D = D; a.eps = eps; a.pieces = fp8_piece_cols(D);
-    return dtype == SVDCACHE_BF16 ? norm_launch<true>(a, s) : norm_launch<false>(a, s);
+    a.ldh = ldh; a.ldx = ldx; a.ldo = ldo; a.ldq = ldq; a.rows = rows; a.cols = D; a.eps = eps; a.pieces = fp8_piece_cols(D);
+    return dtype == SVDCACHE_BF16 ? rows_launch<true, false, true>(a, kMaxCta / 32, s) : rows_launch<false, false, true>(a, kMaxCta / 32, s);
 }
 
 }  // namespace svdc
