@@ -59,6 +59,44 @@ __device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d
     return lo | (hi << 16);
 }
 
+// x / (1 + exp(-2u)) by ex2 and rcp (each good to a few 2^-23): exp(-2u) = 2^(x (a + b x^2)).  Beyond the range of
+// exp the quotient is 0 or x.
+__device__ __forceinline__ float gelu_tanh(float x) {
+    const float t = x * fmaf(x * x, -0.10294324f, -2.3022082f);    // -2 sqrt(2 / pi) log2(e) {0.044715, 1}
+    float e, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(t));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return x * r;
+}
+
+// These kernels are short and follow one another, so each may be launched while the one before it still runs: what
+// does not touch memory of the stream's other work (barriers, tensor memory, descriptors) comes before
+// previous_done(), everything else after it, and next_may_launch() lets the following kernel begin its own such part.
+// previous_done() returns when all earlier work of the stream is complete and visible.
+__device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void next_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+int launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t s, const A &...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const int rc = record_cuda(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+    if (rc) return rc;
+    count_launch();
+    return check_last_launch();
+}
+
 // launches (quant_fp8.cu, gemm_fp8.cu)
 int quantize_fp8_launch(const void *X, int64_t rows, int cols, int64_t ld, int dtype, int tile_rows, void *Q, int64_t ldq,
                         void *S, cudaStream_t s);

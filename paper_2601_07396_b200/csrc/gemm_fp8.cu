@@ -6,10 +6,11 @@
 // 128 rows x 4 groups reaches tensor memory as it is stored (tcgen05.cp), one word per row whose byte g % 4 the
 // four MMAs of group g name.  Sums are fp32 in tensor memory.
 //
-// tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns are up to 256 rows of
-// C, so that few rows of C waste no tensor work.  One CTA per tile and K range; the CTAs of a cluster share a
-// tile, each sums its own K range, and after one cluster barrier each adds up its share of the rows over the
-// cluster in rank order (distributed shared memory): no atomics, the same sum in every run.
+// tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns are up to 128 rows of
+// C, so that few rows of C waste no tensor work.  One CTA per tile; where that leaves SMs idle, the S CTAs of a
+// cluster share a tile: CTA r takes the groups r, r + S, ... of K (together they read whole runs of B's rows), sends
+// every other CTA the rows of its sum that are that one's to finish (stores into its shared memory, then an arrival on
+// its mbarrier), and finishes its own share, adding the parts in rank order: no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
 #include <atomic>
 #include <type_traits>
@@ -43,16 +44,6 @@ struct TileParams {
     int *status;
 };
 
-// x / (1 + exp(-2u)) by ex2 and rcp (each good to a few 2^-23): exp(-2u) = 2^(x (a + b x^2)).  Beyond the range of
-// exp the quotient is 0 or x.
-__device__ __forceinline__ float gelu_tanh(float x) {
-    const float t = x * fmaf(x * x, -0.10294324f, -2.3022082f);    // -2 sqrt(2 / pi) log2(e) {0.044715, 1}
-    float e, r;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(t));
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return x * r;
-}
-
 // four neighbouring columns n .. n + 3 of row m of C (n a multiple of 4): plain types
 __device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int n, const float (&v)[4]) {
     if (p.out == SVDCACHE_F32) {
@@ -73,30 +64,22 @@ __device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int 
     }
 }
 
-// The rows of a tile are dealt to its cluster's S CTAs in equal runs, and within a CTA to the warps, R at a time, four
-// columns per lane: the sum over the cluster in rank order, bias, activation, and out.  R * S loads are in flight.
+// The rows of a tile are dealt to its cluster's S CTAs in runs of tile_m / S, and within a CTA to the warps, R at a
+// time, four columns per lane.  `parts`: S blocks [tile_m / S][128] of sums, one from every CTA.
 template <int S, int R>
-__device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t base, int rank, int64_t m0, int n_tile) {
+__device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t parts, int rank, int64_t m0, int n_tile, const float (&bias)[4]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int per = (p.tile_m + S - 1) / S, r_lo = rank * per;
-    const int r_hi = min(min(r_lo + per, p.tile_m), (int)(p.M - m0 < p.tile_m ? p.M - m0 : p.tile_m));
+    const int per = p.tile_m / S;
+    const int64_t m_first = m0 + rank * per;
+    const int rows = (int)(p.M - m_first < per ? p.M - m_first : per);
     const int n = n_tile * kTileN + 4 * lane;
-    float bias[4] = {0.f, 0.f, 0.f, 0.f};
-    if (p.bias)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < p.N) bias[i] = p.bias[n + i];
-    for (int r0 = r_lo + warp * R; r0 < r_hi; r0 += kTileThreads / 32 * R) {
+    for (int r0 = warp * R; r0 < rows; r0 += kTileThreads / 32 * R) {
         float4 part[R][S];
 #pragma unroll
-        for (int x = 0; x < S; ++x) {
-            const uint32_t from = S == 1 ? base : cluster_addr(base, (uint32_t)x);
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const uint32_t at = from + (uint32_t)(min(r0 + i, p.tile_m - 1) * kTileN + 4 * lane) * 4u;
-                part[i][x] = S == 1 ? shared_load(at) : cluster_load(at);
-            }
-        }
+            for (int x = 0; x < S; ++x)
+                part[i][x] = shared_load(parts + (uint32_t)((x * per + min(r0 + i, per - 1)) * kTileN + 4 * lane) * 4u);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             float v[4] = {part[i][0].x, part[i][0].y, part[i][0].z, part[i][0].w};
@@ -109,8 +92,8 @@ __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t base, 
                 v[j] += bias[j];
                 if (p.act == SVDCACHE_ACT_GELU) v[j] = gelu_tanh(v[j]);
             }
-            const int64_t m = m0 + r0 + i;
-            const bool live = r0 + i < r_hi;
+            const int64_t m = m_first + r0 + i;
+            const bool live = r0 + i < rows;
             if (p.out != SVDCACHE_FP8) {
                 if (live) store_plain(p, m, n, v);
                 continue;
@@ -137,28 +120,44 @@ __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t base, 
     }
 }
 
+// one group of K of the tile into ring slot s
+__device__ __forceinline__ void request_group(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const TileParams &p, uint32_t dst, uint32_t bar,
+                                              int g, bool scales, int64_t m0, int n_tile) {
+    mbar_arrive_expect_tx(bar, kBBytes + p.a_bytes + (scales ? 2 * kScalePieceBytes : 0));
+    tma_load_2d(dst, &tm_b, bar, g * kStageK, n_tile * kTileN);
+    tma_load_2d(dst + kBBytes, &tm_a, bar, g * kStageK, (int)m0);
+    if (scales) {
+        const uint32_t sdst = dst + kBBytes + p.a_bytes;
+        const int64_t at = g / kScaleGroups;
+        bulk_load(sdst, p.SB + ((size_t)n_tile * p.pieces + at) * kScalePieceBytes, kScalePieceBytes, bar);
+        bulk_load(sdst + kScalePieceBytes, p.SA + ((size_t)(m0 / kScaleRows) * p.pieces + at) * kScalePieceBytes, kScalePieceBytes, bar);
+    }
+}
+
 __global__ void __launch_bounds__(kTileThreads)
 tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const TileParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxStages + 1];
+    __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxStages + 2];
     __shared__ uint32_t tmem_slot_mem;
     __shared__ int abort_mem;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    float *stage_f32 = reinterpret_cast<float *>(smem_raw + (base - smem_u32(smem_raw)));
-    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxStages, done_bar = empty + 8 * kMaxStages;
+    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxStages, done_bar = empty + 8 * kMaxStages, parts_bar = done_bar + 8;
     volatile int *abort_flag = &abort_mem;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    const int rank = (int)(blockIdx.x % (unsigned)p.splits);            // = rank in the cluster
-    const int tile = (int)(blockIdx.x / (unsigned)p.splits);
+    const int S = p.splits;
+    const int rank = (int)(blockIdx.x % (unsigned)S);                   // = rank in the cluster
+    const int tile = (int)(blockIdx.x / (unsigned)S);
     const int n_tile = tile % p.n_tiles;
     const int64_t m0 = (int64_t)(tile / p.n_tiles) * p.tile_m;
-    const int n0 = n_tile * kTileN;
-    const int g_lo = (int)((int64_t)p.groups * rank / p.splits), g_hi = (int)((int64_t)p.groups * (rank + 1) / p.splits);
+    const int count = (p.groups - rank + S - 1) / S;                    // groups rank, rank + S, ... of K: at least one
+    // the sums to finish: where the ring was (one CTA per tile: all of its loads have been consumed), or behind it
+    const uint32_t parts = S == 1 ? base : base + (uint32_t)p.stages * p.stage_bytes;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done_bar, 1);
+        mbar_init(parts_bar, 4 * S);                                    // four warps of every CTA
         abort_mem = 0;
         fence_barrier_init();
         prefetch_tensormap(&tm_a);
@@ -168,32 +167,33 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         tmem_alloc(smem_u32(&tmem_slot_mem), (uint32_t)p.tmem_cols);
         tmem_relinquish();
     }
+    __syncwarp();
+    previous_done();
+    // the empty ring is filled before anything else is set up; a piece of scales comes with every group that is the
+    // CTA's first in it
+    if (threadIdx.x == 0)
+        for (int i = 0; i < p.stages && i < count; ++i)
+            request_group(tm_a, tm_b, p, base + i * p.stage_bytes, full + 8 * i, rank + i * S, i == 0 || (rank + i * S) % kScaleGroups < S, m0, n_tile);
     tc_fence_before();
     __syncthreads();
+    next_may_launch();
     tc_fence_after();
+    if (S > 1) cluster_arrive();                                        // this CTA's barriers exist
     const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};                               // of the four columns that finish_rows gives this lane
+    if (p.bias)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n_tile * kTileN + 4 * lane + j < p.N) bias[j] = p.bias[n_tile * kTileN + 4 * lane + j];
 
     if (warp == 0) {
         if (lane == 0) {
             int s = 0;
-            uint32_t ph = 1;
-            const int64_t piece_a = m0 / kScaleRows, last_a = (p.M - 1) / kScaleRows;
-            for (int g = g_lo; g < g_hi; ++g) {
+            uint32_t ph = 0;
+            for (int i = p.stages; i < count; ++i) {
                 if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) break;
-                const uint32_t dst = base + s * p.stage_bytes, bar = full + 8 * s;
-                const bool scales = g == g_lo || (g & (kScaleGroups - 1)) == 0;
-                const int na = scales ? (p.tile_m > kScaleRows && piece_a + 1 <= last_a ? 2 : 1) : 0;
-                mbar_arrive_expect_tx(bar, kBBytes + p.a_bytes + (scales ? (1 + na) * kScalePieceBytes : 0));
-                tma_load_2d(dst, &tm_b, bar, g * kStageK, n0);
-                tma_load_2d(dst + kBBytes, &tm_a, bar, g * kStageK, (int)m0);
-                if (scales) {
-                    const uint32_t sdst = dst + kBBytes + p.a_bytes;
-                    const int64_t at = g / kScaleGroups;
-                    bulk_load(sdst, p.SB + ((size_t)n_tile * p.pieces + at) * kScalePieceBytes, kScalePieceBytes, bar);
-                    for (int i = 0; i < na; ++i)
-                        bulk_load(sdst + (1 + i) * kScalePieceBytes, p.SA + ((size_t)(piece_a + i) * p.pieces + at) * kScalePieceBytes,
-                                  kScalePieceBytes, bar);
-                }
+                const int g = rank + i * S;
+                request_group(tm_a, tm_b, p, base + s * p.stage_bytes, full + 8 * s, g, g % kScaleGroups < S, m0, n_tile);
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
         }
@@ -202,73 +202,79 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         if (lane == 0) {
             int s = 0;
             uint32_t ph = 0;
-            // scale words: four columns for B, then eight for A; two sets that alternate
+            // scale words: four columns for B, then four for A; two sets that alternate
             const uint32_t sf = tmem + (uint32_t)p.tmem_cols - 32u;
-            const uint32_t a_word = (uint32_t)(m0 % kScaleRows) / 32u;   // a tile of fewer than 128 rows may begin inside a piece
+            const uint32_t a_word = (uint32_t)(m0 % kScaleRows) / 32u;   // 0 or 2: a tile of 64 rows may begin in the middle of a piece
             uint32_t set = 1;
-            for (int g = g_lo; g < g_hi; ++g) {
+            for (int i = 0; i < count; ++i) {
+                const int g = rank + i * S;
                 if (!mbar_wait(full + 8 * s, ph, abort_flag, 2)) break;
                 tc_fence_after();
                 const uint32_t src = base + s * p.stage_bytes;
-                if (g == g_lo || (g & (kScaleGroups - 1)) == 0) {
+                if (i == 0 || g % kScaleGroups < S) {
                     set ^= 1u;
                     const uint32_t ssrc = src + kBBytes + p.a_bytes;
                     tmem_cp_scales(sf + 16 * set, smem_desc_scales(ssrc));
                     tmem_cp_scales(sf + 16 * set + 4, smem_desc_scales(ssrc + kScalePieceBytes));
-                    if (p.tile_m > kScaleRows) tmem_cp_scales(sf + 16 * set + 8, smem_desc_scales(ssrc + 2 * kScalePieceBytes));
                 }
                 const uint64_t bd = smem_desc_kmajor(src, 128), ad = smem_desc_kmajor(src + kBBytes, 128);
                 const uint32_t idesc = idesc_mxf8(kTileN, p.tile_m, g & 3);
 #pragma unroll
                 for (int ks = 0; ks < kStageK / 32; ++ks)
                     mma_mxf8_ss(tmem, bd + 2 * ks, ad + 2 * ks, idesc, sf + 16 * set, sf + 16 * set + 4 + a_word,
-                                (g > g_lo || ks > 0) ? 1u : 0u);
+                                (i > 0 || ks > 0) ? 1u : 0u);
                 mma_commit(empty + 8 * s);
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
             mma_commit(done_bar);
         }
         __syncwarp();
-    } else {
-        // accumulator -> shared memory, [row of C][128 columns]: the ring is free once every MMA is done
-        const int q = warp & 3;
+    }
+    // every wait below is passed by all CTAs of the cluster in the same order, also after a time-out in one of them
+    if (S > 1) cluster_wait();                                          // the other CTAs' barriers exist
+    if (warp >= 2) {
+        const int q = warp & 3, shift = 31 - __clz(p.tile_m / S);        // runs of a power of two of rows
         const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(done_bar, 0u, abort_flag, 3));
         tc_fence_after();
-        if (ok && g_hi > g_lo) {
-            for (int c = 0; c < p.tile_m; c += 32) {
-                uint32_t acc[32];
-                tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + c, acc);
-                tmem_wait_ld();
+        for (int c = 0; ok && c < p.tile_m; c += 32) {
+            uint32_t acc[32];
+            tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + c, acc);
+            tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (c + i < p.tile_m) stage_f32[(c + i) * kTileN + q * 32 + lane] = __uint_as_float(acc[i]);
+            for (int i = 0; i < 32; ++i) {
+                if (c + i >= p.tile_m) continue;
+                const int owner = (c + i) >> shift, row = (rank << shift) + (c + i) - (owner << shift);
+                const uint32_t at = parts + (uint32_t)(row * kTileN + q * 32 + lane) * 4u;
+                cluster_store(S > 1 ? cluster_addr(at, (uint32_t)owner) : at, __uint_as_float(acc[i]));
             }
         }
         tc_fence_before();
+        if (S > 1) {
+            __syncwarp();
+            if (lane < S) mbar_arrive_cluster(cluster_addr(parts_bar, (uint32_t)lane));
+        }
     }
     __syncthreads();
-    if (*abort_flag) {
-        // a wait ran out: tell the host, and let what is in flight land before the memory goes
-        if (threadIdx.x == 0) {
-            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
-            const long long t0 = clock64();
-            while (clock64() - t0 < kWaitCycles / 100) {}
-        }
-        __syncthreads();
-    }
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
     }
-    if (p.splits > 1) cluster_sync();
-
-    switch (p.splits) {
-        case 1: finish_rows<1, 4>(p, base, rank, m0, n_tile); break;
-        case 2: finish_rows<2, 4>(p, base, rank, m0, n_tile); break;
-        case 4: finish_rows<4, 4>(p, base, rank, m0, n_tile); break;
-        default: finish_rows<8, 2>(p, base, rank, m0, n_tile); break;
+    if (S > 1 && !mbar_wait_cluster(parts_bar, 0u)) *abort_flag = 5;
+    if (*abort_flag) {
+        // a wait ran out: tell the host, and let what is in flight land before the memory goes
+        if (lane == 0) {
+            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
+            const long long t0 = clock64();
+            while (clock64() - t0 < kWaitCycles / 100) {}
+        }
     }
-    if (p.splits > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
+    __syncwarp();
+    switch (S) {
+        case 1: finish_rows<1, 4>(p, parts, rank, m0, n_tile, bias); break;
+        case 2: finish_rows<2, 4>(p, parts, rank, m0, n_tile, bias); break;
+        case 4: finish_rows<4, 2>(p, parts, rank, m0, n_tile, bias); break;
+        default: finish_rows<8, 1>(p, parts, rank, m0, n_tile, bias); break;
+    }
 }
 
 // ---------------------------------------------------------------------- pairs of CTAs ---
@@ -356,7 +362,7 @@ __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairPara
 }
 
 template <int OUT>
-__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
             const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ CUtensorMap tm_sb,
             const __grid_constant__ CUtensorMap tm_c, const PairParams p) {
@@ -392,6 +398,8 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     __syncthreads();
     cluster_sync();                                  // both CTAs' barriers exist
     tc_fence_after();
+    previous_done();
+    next_may_launch();
     const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
 
     if (warp == 0) {
@@ -657,42 +665,37 @@ int tile_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
     p.act = a.act; p.out = a.out; p.status = a.status;
     p.groups = (int)fp8_groups(a.K); p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
-    p.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
     p.n_tiles = (a.N + kTileN - 1) / kTileN;
-    const int64_t tiles = (a.M + p.tile_m - 1) / p.tile_m * p.n_tiles;
+    auto tiles = [&] { return (a.M + p.tile_m - 1) / p.tile_m * p.n_tiles; };
+    // Rows per tile: what M needs, up to 128, or 64 where that still leaves SMs idle.  (Fewer only where M has no more:
+    // an MMA's scale words begin at an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
+    p.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    if (p.tile_m == 128 && tiles() * 2 <= sms) p.tile_m = 64;
+    // CTAs per tile: until every SM has one, or two where a tile has at most 64 rows and half of the shared memory
+    // still makes a ring; each CTA keeps two groups of K or more.
+    const bool halves = p.tile_m <= 64;
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= sms && p.groups >= 2 * p.splits) p.splits *= 2;
-    if (tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    while (p.splits < 8 && tiles() * p.splits * 2 <= (halves ? 2 * sms : sms) && p.groups >= 4 * p.splits) p.splits *= 2;
+    if (tiles() * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
-    p.stage_bytes = kBBytes + p.a_bytes + (p.a_bytes < 1024 * 32 ? 1024u : 2048u);
-    p.tmem_cols = p.tile_m <= 32 ? 64 : p.tile_m == 64 ? 128 : p.tile_m == 128 ? 256 : 512;
-    int stages = (kSmemLimit - 1024) / (int)p.stage_bytes;
-    if (stages > kMaxStages) stages = kMaxStages;
+    p.stage_bytes = kBBytes + p.a_bytes + 1024u;
+    p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
+    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // one CTA per tile: they pass through the ring
+    const size_t room = halves && tiles() * p.splits > sms ? kSmemLimit / 2 : kSmemLimit;
+    static_assert((kSmemLimit / 2 - 1024 - 64 * kTileN * 4) / (kBBytes + 64 * kStageK + 1024) >= 2 &&
+                  (kSmemLimit - 1024 - 128 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
+    p.stages = (int)((room - 1024 - (p.splits > 1 ? sums : 0)) / p.stage_bytes);
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
     const int longest = (p.groups + p.splits - 1) / p.splits;
-    const int least = (int)(((size_t)p.tile_m * kTileN * 4 + p.stage_bytes - 1) / p.stage_bytes);   // the accumulator passes through the ring
-    if (stages > longest) stages = longest > least ? longest : least;
-    p.stages = stages;
-    const size_t smem = 1024 + (size_t)stages * p.stage_bytes;
+    if (p.stages > longest) p.stages = longest;
+    size_t smem = (size_t)p.stages * p.stage_bytes;
+    smem = 1024 + (p.splits > 1 ? smem + sums : smem > sums ? smem : sums);
 
     CUtensorMap tm_a, tm_b;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
     if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, kTileN);
     if (rc) return rc;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(tiles * p.splits));
-    cfg.blockDim = dim3(kTileThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.splits;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    rc = record_cuda(cudaLaunchKernelEx(&cfg, tile_kernel, tm_a, tm_b, p));
-    if (rc) return rc;
-    count_launch();
-    return check_last_launch();
+    return launch_early(tile_kernel, dim3((unsigned)(tiles() * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p);
 }
 
 // a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
@@ -744,9 +747,7 @@ int pair_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     if (rc) return rc;
     const int clusters = sms / 2 < p.tiles ? sms / 2 : p.tiles;
     auto launch = [&](auto kern) {
-        kern<<<2 * clusters, kPairThreads, kPairSmem, s>>>(tm_a, tm_b, tm_sa, tm_sb, tm_c, p);
-        count_launch();
-        return check_last_launch();
+        return launch_early(kern, dim3(2 * (unsigned)clusters), dim3(kPairThreads), kPairSmem, 2, s, tm_a, tm_b, tm_sa, tm_sb, tm_c, p);
     };
     return a.out == SVDCACHE_FP8 ? launch(pair_kernel<SVDCACHE_FP8>)
            : a.out == SVDCACHE_BF16 ? launch(pair_kernel<SVDCACHE_BF16>) : launch(pair_kernel<SVDCACHE_F32>);

@@ -133,6 +133,8 @@ template <bool BF16, bool CUT, bool NORM, int V> __global__ void __launch_bounds
     const int step0 = (blockIdx.y * a.warps + at) * V, first = (step0 * 32 + lane) * kChunk;   // this lane's columns: first + 256 j
     constexpr int e = BF16 ? 2 : 4;
     float v[V][kChunk];
+    previous_done();
+    next_may_launch();
     {
         Raw<BF16> rh[V], rx[NORM ? V : 1];
         const char *h_row = reinterpret_cast<const char *>(a.H) + (size_t)m * a.ldh * e;
@@ -239,6 +241,8 @@ template <bool BF16, bool CUT> __global__ void __launch_bounds__(kThreads) tiles
     const int g = (int)(blockIdx.x % a.groups), lane = threadIdx.x % kGroupLanes;
     const int c0 = g * kFp8Group + lane * kChunk;
     Raw<BF16> raw[kSteps];
+    previous_done();
+    next_may_launch();
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int64_t m = row0 + i * kRowsAtOnce + threadIdx.x / kGroupLanes;
@@ -291,22 +295,17 @@ template <bool BF16, bool CUT, bool NORM> int rows_launch(RowsArgs a, int most, 
     const int64_t grid = (a.rows + rows_at_once - 1) / rows_at_once;
     const dim3 blocks((unsigned)grid, (unsigned)((steps + a.warps * v - 1) / (a.warps * v))), threads(32 * a.warps * rows_at_once);
     switch (v) {
-        case 1: rows_kernel<BF16, CUT, NORM, 1><<<blocks, threads, 0, s>>>(a); break;
-        case 2: rows_kernel<BF16, CUT, NORM, 2><<<blocks, threads, 0, s>>>(a); break;
-        case 3: rows_kernel<BF16, CUT, NORM, 3><<<blocks, threads, 0, s>>>(a); break;
-        default: rows_kernel<BF16, CUT, NORM, 4><<<blocks, threads, 0, s>>>(a); break;
+        case 1: return launch_early(rows_kernel<BF16, CUT, NORM, 1>, blocks, threads, 0, 1, s, a);
+        case 2: return launch_early(rows_kernel<BF16, CUT, NORM, 2>, blocks, threads, 0, 1, s, a);
+        case 3: return launch_early(rows_kernel<BF16, CUT, NORM, 3>, blocks, threads, 0, 1, s, a);
+        default: return launch_early(rows_kernel<BF16, CUT, NORM, 4>, blocks, threads, 0, 1, s, a);
     }
-    count_launch();
-    return check_last_launch();
 }
 
 template <bool BF16> int tiles_launch(const TilesArgs &a, cudaStream_t s) {
     const int64_t grid = (a.rows + kScaleRows - 1) / kScaleRows * a.groups;
     if (grid > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-    if (a.cols % kChunk) tiles_kernel<BF16, true><<<(unsigned)grid, kThreads, 0, s>>>(a);
-    else tiles_kernel<BF16, false><<<(unsigned)grid, kThreads, 0, s>>>(a);
-    count_launch();
-    return check_last_launch();
+    return launch_early(a.cols % kChunk ? tiles_kernel<BF16, true> : tiles_kernel<BF16, false>, dim3((unsigned)grid), dim3(kThreads), 0, 1, s, a);
 }
 
 }  // namespace

@@ -146,9 +146,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 // ------------------------------------------------------------------- thread-block clusters ---
 // Every thread of every CTA of the cluster arrives once and waits once (shared-memory writes before the
 // arrival are visible to the whole cluster after the wait).
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 // address of the same shared-memory location in CTA `rank` of the cluster
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t saddr, uint32_t rank) {
@@ -161,15 +163,31 @@ __device__ __forceinline__ float4 shared_load(uint32_t addr) {
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ float4 cluster_load(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
-
 // arrival on an mbarrier of another CTA of the cluster (an address from cluster_addr)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Bounded wait for arrivals from the whole cluster and the shared-memory stores before them.  It does not give up when
+// another thread has: whoever else holds this CTA's addresses must be done with them before the CTA leaves.
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    for (uint32_t it = 0;; ++it) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t"
+            ".reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t"
+            "}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((it & 63u) == 63u && clock64() - t0 > 2 * kWaitCycles) return false;
+    }
 }
 
 // ------------------------------------------------ a pair of CTAs working on one tile (cta_group::2) ---
