@@ -24,6 +24,7 @@ using namespace sm100;
 
 namespace {
 
+constexpr int kSmemLimit = 227 * 1024 - 7 * 1024;     // dynamic; the static part of any of the kernels is below 7 KB
 constexpr int kTileN = 128;                           // columns of C per tile: MMA M
 constexpr int kStageK = 128;                          // bytes of K per pipeline stage: one scale group
 constexpr uint32_t kBBytes = kTileN * kStageK;
@@ -143,7 +144,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxStages, done_bar = empty + 8 * kMaxStages, parts_bar = done_bar + 8;
     volatile int *abort_flag = &abort_mem;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
     const int S = p.splits;
     const int rank = (int)(blockIdx.x % (unsigned)S);                   // = rank in the cluster
@@ -154,7 +155,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     // the sums to finish: where the ring was (one CTA per tile: all of its loads have been consumed), or behind it
     const uint32_t parts = S == 1 ? base : base + (uint32_t)p.stages * p.stage_bytes;
 
-    if (threadIdx.x == 0) {
+    if (warp == 0 && elect_one()) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done_bar, 1);
         mbar_init(parts_bar, 4 * S);                                    // four warps of every CTA
@@ -171,7 +172,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     previous_done();
     // the empty ring is filled before anything else is set up; a piece of scales comes with every group that is the
     // CTA's first in it
-    if (threadIdx.x == 0)
+    if (warp == 0 && elect_one())
         for (int i = 0; i < p.stages && i < count; ++i)
             request_group(tm_a, tm_b, p, base + i * p.stage_bytes, full + 8 * i, rank + i * S, i == 0 || (rank + i * S) % kScaleGroups < S, m0, n_tile);
     tc_fence_before();
@@ -187,7 +188,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             if (n_tile * kTileN + 4 * lane + j < p.N) bias[j] = p.bias[n_tile * kTileN + 4 * lane + j];
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0;
             uint32_t ph = 0;
             for (int i = p.stages; i < count; ++i) {
@@ -199,7 +200,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0;
             uint32_t ph = 0;
             // scale words: four columns for B, then four for A; two sets that alternate
@@ -279,25 +280,38 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
 
 // ---------------------------------------------------------------------- pairs of CTAs ---
 //
-// pair_kernel: a persistent cluster of two CTAs computes tiles of 256 x 256 of C with cta_group::2 MMAs: each CTA
+// pair_kernel: a persistent cluster of two CTAs computes tiles of 256 x BN of C with cta_group::2 MMAs: each CTA
 // holds 128 rows of the tile in its tensor memory and loads its 128 rows of A and half of the tile's rows of B, so
-// a group of K costs an SM 32 KB instead of the 48 KB of a one-CTA 128 x 256 tile -- the traffic between L2 and
-// the SMs is what bounds such a kernel first.
-// Tensor memory (512 columns): two accumulators of 256 columns that share 32, columns [0, 256) and [224, 480), and
-// two sets of scale words in the last 32.  The epilogue reads the shared columns first, and the MMAs of the next
-// tile start as soon as they are read.
-// Warps: 0 TMA producer, 1 MMA issuer (the first CTA's, for both), 2-5 and 6-9 the two column halves of the tile.
+// a group of K costs an SM 32 KB at BN = 256 instead of the 48 KB of a one-CTA 128 x 256 tile -- the traffic between
+// L2 and the SMs is what bounds such a kernel first.
+// Tensor memory (512 columns) holds two accumulators, so that a tile's epilogue runs beside the next tile's MMAs, and two
+// sets of scale words in the last 32 columns.
+//   BN = 128, 192   accumulators side by side; the two epilogue groups (warps 2-5, 6-9) take alternate tiles
+//   BN = 256        only for 8-bit C, whose groups of 128 columns a tile of 192 would cut: columns [0, 256) and
+//                   [224, 480) share 32, the groups take the two column halves of every tile, read the shared columns
+//                   first, and the next tile's MMAs start as soon as these are read (about 1000 cycles a tile)
+// Warps: 0 TMA producer, 1 MMA issuer (the first CTA's, for both), 2-9 epilogue.
 
-constexpr int kPairM = 256, kPairN = 256;
+constexpr int kPairM = 256;
 constexpr int kPairThreads = 320;
-constexpr int kPairStages = 5;
-constexpr uint32_t kPairABytes = 128 * kStageK, kPairBBytes = 128 * kStageK;      // each CTA's share
-constexpr uint32_t kPairScaleBytes = 3 * kScalePieceBytes;                        // own rows of A, all 256 of B
-constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes + 2048;
+constexpr uint32_t kPairABytes = 128 * kStageK;                                   // each CTA's share
 constexpr uint32_t kStoreBytes = 32 * 128;                                        // a warp's box of C: 32 rows of 128 bytes
-constexpr uint32_t kPairSmem = 1024 + kPairStages * kPairStageBytes + 8 * kStoreBytes;
-static_assert(kPairSmem <= 222 * 1024, "dynamic shared memory");
-constexpr uint32_t kAccStep = 224, kScaleCol = 480;
+constexpr uint32_t kScaleCol = 480;
+constexpr int kMaxPairStages = 7;
+
+template <int BN> struct Pair {
+    static constexpr bool kHalves = BN == 256;
+    static constexpr uint32_t kBBytes = BN / 2 * kStageK;                         // each CTA's share
+    static constexpr int kBPieces = (BN + 127) / 128;                             // of scales: all rows of B, in both CTAs
+    static constexpr uint32_t kScaleBytes = (1 + kBPieces) * kScalePieceBytes;
+    static constexpr uint32_t kStageBytes = (kPairABytes + kBBytes + kScaleBytes + 1023) / 1024 * 1024;
+    static constexpr int kFit = (int)((kSmemLimit - 1024 - 8 * kStoreBytes) / kStageBytes);
+    static constexpr int kStages = kFit < kMaxPairStages ? kFit : kMaxPairStages;
+    static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + 8 * kStoreBytes;
+    static constexpr uint32_t kAccStep = kHalves ? 224 : BN;
+    static constexpr int kWarpCols = kHalves ? 128 : BN;                          // columns of a tile that a warp finishes
+    static_assert(kStages >= 4 && (BN == 256 || 2 * BN <= (int)kScaleCol), "shared and tensor memory");
+};
 constexpr int kRasterRows = 8;      // tile rows that neighbouring clusters share: 8 x n tiles are walked column by column
 
 struct PairParams {
@@ -361,27 +375,31 @@ __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairPara
     __syncwarp();
 }
 
-template <int OUT>
+template <int OUT, int BN>
 __global__ void __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
             const __grid_constant__ CUtensorMap tm_sa, const __grid_constant__ CUtensorMap tm_sb,
             const __grid_constant__ CUtensorMap tm_c, const PairParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) unsigned long long bar_mem[2 * kPairStages + 2];
-    __shared__ __align__(16) float bias_mem[8][kPairN / 2];
+    using T = Pair<BN>;
+    constexpr bool kHalves = T::kHalves;
+    __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxPairStages + 4];
+    __shared__ __align__(16) float bias_mem[8][T::kWarpCols];
     __shared__ uint32_t tmem_slot_mem;
     __shared__ int abort_mem;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kPairStages, acc_full = empty + 8 * kPairStages, acc_empty = acc_full + 8;
+    const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxPairStages, acc_full = empty + 8 * kMaxPairStages, acc_empty = acc_full + 16;
     volatile int *abort_flag = &abort_mem;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x & 1u;           // in the cluster
     const int cluster = (int)(blockIdx.x >> 1), clusters = (int)(gridDim.x >> 1);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kPairStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-        mbar_init(acc_full, 1);
-        mbar_init(acc_empty, 16);                    // the epilogue warps of both CTAs
+        for (int s = 0; s < T::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int i = 0; i < 2; ++i) {                // halves: the first of each serves both accumulators in turn
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, kHalves ? 16 : 8);   // the epilogue warps of both CTAs that read it
+        }
         abort_mem = 0;
         fence_barrier_init();
         prefetch_tensormap(&tm_a);
@@ -403,90 +421,102 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             int s = 0;
             uint32_t ph = 1;
             for (int t = cluster; t < p.tiles; t += clusters) {
                 const TileAt at = pair_tile(p, t);
-                const int row_a = at.m * kPairM + (int)rank * 128, row_b = at.n * kPairN + (int)rank * 128;
+                const int row_a = at.m * kPairM + (int)rank * 128, row_b = at.n * BN + (int)rank * (BN / 2);
                 for (int g = 0; g < p.groups; ++g) {
                     if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) goto done;
-                    const uint32_t dst = base + s * kPairStageBytes, bar = cluster_addr(full + 8 * s, 0);
+                    const uint32_t dst = base + s * T::kStageBytes, bar = cluster_addr(full + 8 * s, 0);
                     const bool scales = (g & (kScaleGroups - 1)) == 0;
                     if (rank == 0)
-                        mbar_arrive_expect_tx(full + 8 * s, 2 * (kPairABytes + kPairBBytes + (scales ? kPairScaleBytes : 0)));
+                        mbar_arrive_expect_tx(full + 8 * s, 2 * (kPairABytes + T::kBBytes + (scales ? T::kScaleBytes : 0)));
                     tma_load_2d_pair(dst, &tm_a, bar, g * kStageK, row_a);
                     tma_load_2d_pair(dst + kPairABytes, &tm_b, bar, g * kStageK, row_b);
                     if (scales) {
                         // the scale buffers as rows of pieces, g / 4 the piece of the row
-                        const uint32_t sdst = dst + kPairABytes + kPairBBytes;
+                        const uint32_t sdst = dst + kPairABytes + T::kBBytes;
                         const int c = g / kScaleGroups * (kScalePieceBytes / 4);
                         tma_load_2d_pair(sdst, &tm_sa, bar, c, at.m * 2 + (int)rank);
-                        tma_load_2d_pair(sdst + kScalePieceBytes, &tm_sb, bar, c, at.n * 2);
-                        tma_load_2d_pair(sdst + 2 * kScalePieceBytes, &tm_sb, bar, c, at.n * 2 + 1);
+#pragma unroll
+                        for (int i = 0; i < T::kBPieces; ++i)
+                            tma_load_2d_pair(sdst + (1 + i) * kScalePieceBytes, &tm_sb, bar, c, at.n * BN / 128 + i);
                     }
-                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                    if (++s == T::kStages) { s = 0; ph ^= 1u; }
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             int s = 0;
             uint32_t ph = 0, it = 0, set = 1;
             for (int t = cluster; t < p.tiles; t += clusters, ++it) {
-                if (it > 0 && !mbar_wait(acc_empty, (it - 1) & 1u, abort_flag, 2)) goto done;
+                const uint32_t b = it & 1u;
+                if (kHalves) {
+                    if (it > 0 && !mbar_wait(acc_empty, b ^ 1u, abort_flag, 2)) goto done;
+                } else {
+                    if (it > 1 && !mbar_wait(acc_empty + 8 * b, (it >> 1 & 1u) ^ 1u, abort_flag, 2)) goto done;
+                }
                 tc_fence_after();
-                const uint32_t acc = tmem + (it & 1u) * kAccStep;
+                const uint32_t acc = tmem + b * T::kAccStep;
+                const uint32_t b_word = BN == 192 ? (uint32_t)(pair_tile(p, t).n & 1) * 2u : 0u;   // a tile of 192 may begin in the middle of a piece
                 for (int g = 0; g < p.groups; ++g) {
                     if (!mbar_wait(full + 8 * s, ph, abort_flag, 3)) goto done;
                     tc_fence_after();
-                    const uint32_t src = base + s * kPairStageBytes;
+                    const uint32_t src = base + s * T::kStageBytes;
                     if ((g & (kScaleGroups - 1)) == 0) {
                         set ^= 1u;
-                        const uint32_t ssrc = src + kPairABytes + kPairBBytes, sf = tmem + kScaleCol + 16 * set;
-                        tmem_cp_scales_pair(sf, smem_desc_scales(ssrc));
-                        tmem_cp_scales_pair(sf + 4, smem_desc_scales(ssrc + kScalePieceBytes));
-                        tmem_cp_scales_pair(sf + 8, smem_desc_scales(ssrc + 2 * kScalePieceBytes));
+                        const uint32_t ssrc = src + kPairABytes + T::kBBytes, sf = tmem + kScaleCol + 16 * set;
+#pragma unroll
+                        for (int i = 0; i <= T::kBPieces; ++i) tmem_cp_scales_pair(sf + 4 * i, smem_desc_scales(ssrc + i * kScalePieceBytes));
                     }
                     const uint32_t sf = tmem + kScaleCol + 16 * set;
                     const uint64_t ad = smem_desc_kmajor(src, 128), bd = smem_desc_kmajor(src + kPairABytes, 128);
-                    const uint32_t idesc = idesc_mxf8(kPairM, kPairN, g & 3);
+                    const uint32_t idesc = idesc_mxf8(kPairM, BN, g & 3);
 #pragma unroll
                     for (int ks = 0; ks < kStageK / 32; ++ks)
-                        mma_mxf8_ss_pair(acc, ad + 2 * ks, bd + 2 * ks, idesc, sf, sf + 4, (g > 0 || ks > 0) ? 1u : 0u);
+                        mma_mxf8_ss_pair(acc, ad + 2 * ks, bd + 2 * ks, idesc, sf, sf + 4 + b_word, (g > 0 || ks > 0) ? 1u : 0u);
                     mma_commit_pair(empty + 8 * s);
-                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                    if (++s == T::kStages) { s = 0; ph ^= 1u; }
                 }
-                mma_commit_pair(acc_full);
+                mma_commit_pair(acc_full + (kHalves ? 0 : 8 * b));
             }
         }
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t store = base + kPairStages * kPairStageBytes + (uint32_t)(warp - 2) * kStoreBytes;
+        const int q = warp & 3, group = (warp - 2) >> 2;
+        const uint32_t store = base + T::kStages * T::kStageBytes + (uint32_t)(warp - 2) * kStoreBytes;
         const uint32_t store_row = store + (uint32_t)lane * 128u;
         float *bias = bias_mem[warp - 2];
-        const uint32_t acc_empty_first = cluster_addr(acc_empty, 0);
+        const uint32_t acc_empty_first = cluster_addr(acc_empty + (kHalves ? 0 : 8 * group), 0);
         constexpr int kCols = OUT == SVDCACHE_FP8 ? 128 : OUT == SVDCACHE_BF16 ? 64 : 32;   // columns of C in 128 bytes
+        constexpr int kBlocks = T::kWarpCols / 32;                                          // column blocks of a tensor-memory load
         uint32_t it = 0;
         for (int t = cluster; t < p.tiles; t += clusters, ++it) {
+            if (!kHalves && (int)(it & 1u) != group) continue;
             const TileAt at = pair_tile(p, t);
             const int64_t row0 = (int64_t)at.m * kPairM + rank * 128 + q * 32;
-            const int col0 = at.n * kPairN + half * 128;
+            const int col0 = at.n * BN + (kHalves ? group * 128 : 0);
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kBlocks; ++j) {
                 const int n = col0 + j * 32 + lane;
                 bias[j * 32 + lane] = p.bias && n < p.N ? p.bias[n] : 0.0f;
             }
             __syncwarp();
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full, it & 1u, abort_flag, 4))) goto done;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full + (kHalves ? 0 : 8 * group), (kHalves ? it : it >> 1) & 1u, abort_flag, 4))) goto done;
             tc_fence_after();
-            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (it & 1u) * kAccStep + half * 128;
-            // the columns that the next accumulator shares: the last 32 of the first one, the first 32 of the second
-            const bool shares = half == (int)((it & 1u) ^ 1u);
-            if (!shares && lane == 0) mbar_arrive_cluster(acc_empty_first);
-            // column blocks of 32, the shared one first
-            const int first = shares && half == 1 ? 3 : 0;
+            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (it & 1u) * T::kAccStep + (kHalves ? group * 128 : 0);
+            // halves: the columns that the next accumulator shares are the last 32 of the first one and the first 32 of
+            // the second; the group that does not hold them has nothing to release
+            const bool shares = kHalves && group == (int)((it & 1u) ^ 1u);
+            auto release = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acc_empty_first);
+            };
+            if (kHalves && !shares) release();
             if constexpr (OUT == SVDCACHE_FP8) {
                 float v[128];
 #pragma unroll
@@ -497,11 +527,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                     for (int i = 0; i < 32; ++i) v[j * 32 + i] = __uint_as_float(r[i]);
                 }
                 tmem_wait_ld();
-                tc_fence_before();
-                if (shares) {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(acc_empty_first);
-                }
+                if (!kHalves || shares) release();
                 float top = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) add_bias_and_act<32>(v + 32 * j, bias + 32 * j, p.act);
@@ -532,36 +558,29 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                         const int k = c * 16 + i * 4;
                         w[i] = fp8_pack4(v[k] * inv, v[k + 1] * inv, v[k + 2] * inv, v[k + 3] * inv);
                     }
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                 ::"r"(store_row + (uint32_t)(c ^ (lane & 7)) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    shared_store(store_row + (uint32_t)(c ^ (lane & 7)) * 16u, w);
                 }
                 if (row0 + lane < p.M && col0 < p.N) p.SC[fp8_scale_offset(row0 + lane, col0 / kFp8Group, p.pieces_c)] = (uint8_t)byte;
                 send_box<uint8_t>(&tm_c, p, store, col0, row0, lane);
             } else {
 #pragma unroll 1
-                for (int jj = 0; jj < 4; ++jj) {
-                    // bf16 boxes hold two blocks: 0 1 | 2 3, or 3 2 | 1 0
-                    const int j = first ? 3 - jj : jj;
+                for (int j = 0; j < kBlocks; ++j) {
                     uint32_t r[32];
                     tmem_ld_32x32(acc + j * 32, r);
                     tmem_wait_ld();
-                    if (jj == 0 && shares) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(acc_empty_first);
-                    }
+                    if (j == kBlocks - 1) release();
                     float v[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
                     add_bias_and_act<32>(v, bias + j * 32, p.act);
-                    constexpr int kBlocks = kCols / 32;       // blocks per box
-                    if (jj % kBlocks == 0) {
+                    constexpr int kPerBox = kCols / 32;       // blocks per box
+                    if (j % kPerBox == 0) {
                         if (lane == 0) tma_store_wait_read<0>();
                         __syncwarp();
                     }
-                    const int c0 = kBlocks == 2 ? (j & 1) * 4 : 0;
+                    const int c0 = j % kPerBox * 4;
 #pragma unroll
-                    for (int c = 0; c < 8 / kBlocks; ++c) {
+                    for (int c = 0; c < 8 / kPerBox; ++c) {
                         uint32_t w[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -572,15 +591,12 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                                 w[i] = __float_as_uint(v[c * 4 + i]);
                             }
                         }
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                     ::"r"(store_row + (uint32_t)((c0 + c) ^ (lane & 7)) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                        shared_store(store_row + (uint32_t)((c0 + c) ^ (lane & 7)) * 16u, w);
                     }
-                    if (jj % kBlocks == kBlocks - 1) {
+                    if (j % kPerBox == kPerBox - 1)
                         send_box<typename std::conditional<OUT == SVDCACHE_BF16, __nv_bfloat16, float>::type>(
-                            &tm_c, p, store, col0 + j / kBlocks * kCols, row0, lane);
-                    }
+                            &tm_c, p, store, col0 + j / kPerBox * kCols, row0, lane);
                 }
-                tc_fence_before();
             }
         }
         if (lane == 0) tma_store_wait<0>();
@@ -640,26 +656,58 @@ int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t l
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
-// What the launches ask of the current device, asked once per device: its SMs, and leave for its kernels to
-// use more dynamic shared memory than the default (up to kSmemLimit).
-constexpr int kSmemLimit = 227 * 1024 - 5 * 1024;    // the static part of any of the kernels is below 5 KB
+// What the launches ask of a device, once: its SMs, how many clusters of 1, 2, 4, 8 CTAs of tile_kernel it runs at the
+// same time with all or half of an SM's shared memory per CTA, and leave to use that much.
+struct Device {
+    int sms, clusters[2][4];
+};
 constexpr int kMaxDevices = 64;
 
-int device_ready(int *sms) {
-    static std::atomic<int> known[kMaxDevices];
+int ask_device(Device *d) {
     int dev = 0;
     int rc = record_cuda(cudaGetDevice(&dev));
-    if (rc) return rc;
-    if (dev < kMaxDevices && (*sms = known[dev].load(std::memory_order_acquire)) > 0) return SVDCACHE_OK;
-    rc = record_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
-    for (const void *k : {(const void *)tile_kernel, (const void *)pair_kernel<SVDCACHE_F32>, (const void *)pair_kernel<SVDCACHE_BF16>,
-                          (const void *)pair_kernel<SVDCACHE_FP8>})
+    if (!rc) rc = record_cuda(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev));
+    for (const void *k : {(const void *)tile_kernel, (const void *)pair_kernel<SVDCACHE_F32, 128>, (const void *)pair_kernel<SVDCACHE_F32, 192>,
+                          (const void *)pair_kernel<SVDCACHE_BF16, 128>, (const void *)pair_kernel<SVDCACHE_BF16, 192>,
+                          (const void *)pair_kernel<SVDCACHE_FP8, 128>, (const void *)pair_kernel<SVDCACHE_FP8, 256>})
         if (!rc) rc = record_cuda(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-    if (!rc && dev < kMaxDevices) known[dev].store(*sms, std::memory_order_release);
+    for (int half = 0; half < 2; ++half)
+        for (int i = 0; i < 4 && !rc; ++i) {
+            cudaLaunchConfig_t cfg{};
+            cudaLaunchAttribute attr[1];
+            cfg.gridDim = dim3(8 * (unsigned)d->sms);
+            cfg.blockDim = dim3(kTileThreads);
+            cfg.dynamicSmemBytes = kSmemLimit >> half;
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 1u << i;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            rc = record_cuda(cudaOccupancyMaxActiveClusters(&d->clusters[half][i], tile_kernel, &cfg));
+        }
     return rc;
 }
 
-int tile_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
+int device(Device *d) {
+    static Device known[kMaxDevices];
+    static std::atomic<int> state[kMaxDevices];      // 0: not asked, 1: one thread is asking, 2: known
+    int dev = 0;
+    int rc = record_cuda(cudaGetDevice(&dev));
+    if (rc) return rc;
+    if (dev < kMaxDevices && state[dev].load(std::memory_order_acquire) == 2) {
+        *d = known[dev];
+        return SVDCACHE_OK;
+    }
+    rc = ask_device(d);
+    int zero = 0;
+    if (!rc && dev < kMaxDevices && state[dev].compare_exchange_strong(zero, 1)) {
+        known[dev] = *d;
+        state[dev].store(2, std::memory_order_release);
+    }
+    return rc;
+}
+
+int tile_launch(const GemmFp8Args &a, const Device &d, cudaStream_t s) {
     TileParams p{};
     p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
@@ -670,18 +718,18 @@ int tile_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     // Rows per tile: what M needs, up to 128, or 64 where that still leaves SMs idle.  (Fewer only where M has no more:
     // an MMA's scale words begin at an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
     p.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-    if (p.tile_m == 128 && tiles() * 2 <= sms) p.tile_m = 64;
-    // CTAs per tile: until every SM has one, or two where a tile has at most 64 rows and half of the shared memory
-    // still makes a ring; each CTA keeps two groups of K or more.
+    if (p.tile_m == 128 && tiles() * 2 <= d.sms) p.tile_m = 64;
+    // CTAs per tile: as many as keep two groups of K each, while all clusters still run at the same time: with one CTA
+    // an SM, or two where a tile has at most 64 rows, for which half of the shared memory still makes a ring.
     const bool halves = p.tile_m <= 64;
     p.splits = 1;
-    while (p.splits < 8 && tiles() * p.splits * 2 <= (halves ? 2 * sms : sms) && p.groups >= 4 * p.splits) p.splits *= 2;
+    for (int i = 1; i < 4 && tiles() <= d.clusters[halves][i] && p.groups >= 2 << i; ++i) p.splits = 1 << i;
     if (tiles() * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + 1024u;
     p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
     const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // one CTA per tile: they pass through the ring
-    const size_t room = halves && tiles() * p.splits > sms ? kSmemLimit / 2 : kSmemLimit;
+    const size_t room = halves && tiles() > d.clusters[0][31 - __builtin_clz((unsigned)p.splits)] ? kSmemLimit / 2 : kSmemLimit;
     static_assert((kSmemLimit / 2 - 1024 - 64 * kTileN * 4) / (kBBytes + 64 * kStageK + 1024) >= 2 &&
                   (kSmemLimit - 1024 - 128 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
     p.stages = (int)((room - 1024 - (p.splits > 1 ? sums : 0)) / p.stage_bytes);
@@ -729,10 +777,10 @@ int out_map(CUtensorMap *m, const GemmFp8Args &a) {
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
-int pair_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
+template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, cudaStream_t s) {
     PairParams p{};
     p.M = a.M; p.N = a.N; p.groups = (int)fp8_groups(a.K); p.C = a.C; p.ldc = a.ldc;
-    p.n_tiles = (a.N + kPairN - 1) / kPairN;
+    p.n_tiles = (a.N + BN - 1) / BN;
     const int64_t m_tiles = (a.M + kPairM - 1) / kPairM;
     if (m_tiles * p.n_tiles > 0x3FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.m_tiles = (int)m_tiles;
@@ -740,27 +788,39 @@ int pair_launch(const GemmFp8Args &a, int sms, cudaStream_t s) {
     p.bias = a.bias; p.SC = (uint8_t *)a.SC; p.pieces_c = fp8_piece_cols(a.N); p.act = a.act; p.status = a.status;
     CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_c;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, 128);
-    if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, 128);
+    if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, BN / 2);
     if (!rc) rc = scale_map(&tm_sa, a.SA, a.M, fp8_piece_cols(a.K));
     if (!rc) rc = scale_map(&tm_sb, a.SB, a.N, fp8_piece_cols(a.K));
     if (!rc) rc = out_map(&tm_c, a);
     if (rc) return rc;
-    const int clusters = sms / 2 < p.tiles ? sms / 2 : p.tiles;
-    auto launch = [&](auto kern) {
-        return launch_early(kern, dim3(2 * (unsigned)clusters), dim3(kPairThreads), kPairSmem, 2, s, tm_a, tm_b, tm_sa, tm_sb, tm_c, p);
+    if (clusters > p.tiles) clusters = p.tiles;
+    return launch_early(pair_kernel<OUT, BN>, dim3(2 * (unsigned)clusters), dim3(kPairThreads), Pair<BN>::kSmem, 2, s, tm_a, tm_b, tm_sa,
+                        tm_sb, tm_c, p);
+}
+
+// The wider tile where it takes less time: rounds of the clusters x cycles of a tile's MMAs (a pair's MMA of K = 32
+// measured 105 cycles at BN = 128, 136 at 192 and 182 at 256, where a tile also waits ~1000 cycles for its accumulator).
+int pair_dispatch(const GemmFp8Args &a, int sms, cudaStream_t s) {
+    const int clusters = sms / 2;
+    const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, mmas = fp8_groups(a.K) * 4;
+    auto cost = [&](int bn, int64_t cycles, int64_t more) {
+        return (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters * (mmas * cycles + more);
     };
-    return a.out == SVDCACHE_FP8 ? launch(pair_kernel<SVDCACHE_FP8>)
-           : a.out == SVDCACHE_BF16 ? launch(pair_kernel<SVDCACHE_BF16>) : launch(pair_kernel<SVDCACHE_F32>);
+    if (a.out == SVDCACHE_FP8)
+        return cost(256, 182, 1000) < cost(128, 105, 0) ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
+    const bool wide = cost(192, 136, 0) < cost(128, 105, 0);
+    if (a.out == SVDCACHE_BF16) return wide ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
+    return wide ? pair_launch<SVDCACHE_F32, 192>(a, clusters, s) : pair_launch<SVDCACHE_F32, 128>(a, clusters, s);
 }
 
 }  // namespace
 
 int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
-    int sms = 0;
-    const int rc = device_ready(&sms);
+    Device d;
+    const int rc = device(&d);
     if (rc) return rc;
-    if (a.M > 256 && a.N > 256) return pair_launch(a, sms, s);
-    return tile_launch(a, sms, s);
+    if (a.M > 256 && a.N > 256) return pair_dispatch(a, d.sms, s);
+    return tile_launch(a, d, s);
 }
 
 }  // namespace svdc
