@@ -60,12 +60,13 @@ __device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d
 }
 
 // x / (1 + exp(-2u)) by ex2 and rcp (each good to a few 2^-23): exp(-2u) = 2^(x (a + b x^2)).  Beyond the range of
-// exp the quotient is 0 or x.
+// exp the quotient is 0 or x.  The ftz forms are one instruction each; what they flush (exp below 2^-126 beside the 1, a
+// quotient below |x| 2^-126) is far below the sum's own rounding.
 __device__ __forceinline__ float gelu_tanh(float x) {
     const float t = x * fmaf(x * x, -0.10294324f, -2.3022082f);    // -2 sqrt(2 / pi) log2(e) {0.044715, 1}
     float e, r;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(t));
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return x * r;
 }
 
