@@ -707,29 +707,45 @@ int device(Device *d) {
     return rc;
 }
 
-int tile_launch(const GemmFp8Args &a, const Device &d, cudaStream_t s) {
+// How tile_kernel would take a product.
+struct TilePlan {
+    int tile_m, splits, n_tiles, groups;
+    int64_t tiles;
+    bool shared_sm;          // more CTAs than SMs: half of the shared memory each
+};
+
+TilePlan plan_tile(const GemmFp8Args &a, const Device &d) {
+    TilePlan t{};
+    t.groups = (int)fp8_groups(a.K);
+    t.n_tiles = (a.N + kTileN - 1) / kTileN;
+    // Rows per tile: what M needs, up to 128, or 64 where that still leaves SMs idle.  (Fewer only where M has no more:
+    // an MMA's scale words begin at an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
+    t.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+    if (t.tile_m == 128 && (a.M + 127) / 128 * t.n_tiles * 2 <= d.sms) t.tile_m = 64;
+    t.tiles = (a.M + t.tile_m - 1) / t.tile_m * t.n_tiles;
+    // CTAs per tile: as many as keep two groups of K each, while all clusters still run at the same time: with one CTA
+    // an SM, or two where a tile has at most 64 rows, for which half of the shared memory still makes a ring.
+    const bool halves = t.tile_m <= 64;
+    int log = 0;
+    while (log < 3 && t.tiles <= d.clusters[halves][log + 1] && t.groups >= 4 << log) ++log;
+    t.splits = 1 << log;
+    t.shared_sm = halves && t.tiles > d.clusters[0][log];
+    return t;
+}
+
+int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     TileParams p{};
     p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
     p.act = a.act; p.out = a.out; p.status = a.status;
-    p.groups = (int)fp8_groups(a.K); p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
-    p.n_tiles = (a.N + kTileN - 1) / kTileN;
-    auto tiles = [&] { return (a.M + p.tile_m - 1) / p.tile_m * p.n_tiles; };
-    // Rows per tile: what M needs, up to 128, or 64 where that still leaves SMs idle.  (Fewer only where M has no more:
-    // an MMA's scale words begin at an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
-    p.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-    if (p.tile_m == 128 && tiles() * 2 <= d.sms) p.tile_m = 64;
-    // CTAs per tile: as many as keep two groups of K each, while all clusters still run at the same time: with one CTA
-    // an SM, or two where a tile has at most 64 rows, for which half of the shared memory still makes a ring.
-    const bool halves = p.tile_m <= 64;
-    p.splits = 1;
-    for (int i = 1; i < 4 && tiles() <= d.clusters[halves][i] && p.groups >= 2 << i; ++i) p.splits = 1 << i;
-    if (tiles() * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    p.groups = t.groups; p.splits = t.splits; p.n_tiles = t.n_tiles; p.tile_m = t.tile_m;
+    p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
+    if (t.tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + 1024u;
     p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
     const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // one CTA per tile: they pass through the ring
-    const size_t room = halves && tiles() > d.clusters[0][31 - __builtin_clz((unsigned)p.splits)] ? kSmemLimit / 2 : kSmemLimit;
+    const size_t room = t.shared_sm ? kSmemLimit / 2 : kSmemLimit;
     static_assert((kSmemLimit / 2 - 1024 - 64 * kTileN * 4) / (kBBytes + 64 * kStageK + 1024) >= 2 &&
                   (kSmemLimit - 1024 - 128 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
     p.stages = (int)((room - 1024 - (p.splits > 1 ? sums : 0)) / p.stage_bytes);
@@ -743,7 +759,7 @@ int tile_launch(const GemmFp8Args &a, const Device &d, cudaStream_t s) {
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
     if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, kTileN);
     if (rc) return rc;
-    return launch_early(tile_kernel, dim3((unsigned)(tiles() * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p);
+    return launch_early(tile_kernel, dim3((unsigned)(t.tiles * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p);
 }
 
 // a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
@@ -798,19 +814,33 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
                         tm_sb, tm_c, p);
 }
 
-// The wider tile where it takes less time: rounds of the clusters x cycles of a tile's MMAs (a pair's MMA of K = 32
-// measured 105 cycles at BN = 128, 136 at 192 and 182 at 256, where a tile also waits ~1000 cycles for its accumulator).
-int pair_dispatch(const GemmFp8Args &a, int sms, cudaStream_t s) {
-    const int clusters = sms / 2;
-    const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, mmas = fp8_groups(a.K) * 4;
-    auto cost = [&](int bn, int64_t cycles, int64_t more) {
-        return (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters * (mmas * cycles + more);
-    };
-    if (a.out == SVDCACHE_FP8)
-        return cost(256, 182, 1000) < cost(128, 105, 0) ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
-    const bool wide = cost(192, 136, 0) < cost(128, 105, 0);
-    if (a.out == SVDCACHE_BF16) return wide ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
-    return wide ? pair_launch<SVDCACHE_F32, 192>(a, clusters, s) : pair_launch<SVDCACHE_F32, 128>(a, clusters, s);
+// Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured:
+//   pairs       4.1 us from launch to end, and per round of the clusters and group of K the time of a tile's MMAs: 0.18 us at
+//               BN = 128, 0.21 at 192, 0.33 at 256 (its wait for the accumulator included)
+//   small tiles 5.7 us, 1 more where a cluster has fewer than 8 CTAs, and per group of a CTA's share of K 0.3 us, or 0.5
+//               where CTAs share SMs or their count exceeds them
+// (K = 12288, N = 1152, M = 64 / 256 / 1024: 21.9 / 22.9 / 23.2 us by pairs, 9.9 / 19.1 / 29.3 by small tiles; K = 1152,
+// N = 3072, M = 100 / 1024: 5.9 / 8.0 by pairs, 8.1 / 23.2 by small tiles.)  Up to 64 rows a pair's tile would be mostly
+// empty and its ring too short for weights from memory (1 x 18432 x 3072: 25.8 us by pairs, 13.4 by small tiles).
+struct PairPlan {
+    int bn;
+    int64_t time;
+};
+
+PairPlan plan_pair(const GemmFp8Args &a, const Device &d) {
+    const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, groups = fp8_groups(a.K), clusters = d.sms / 2;
+    auto time = [&](int bn, int64_t group) { return 410 + (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters * groups * group; };
+    const int wide = a.out == SVDCACHE_FP8 ? 256 : 192;
+    const int64_t t_wide = time(wide, wide == 256 ? 33 : 21), t_128 = time(128, 18);
+    return t_wide < t_128 ? PairPlan{wide, t_wide} : PairPlan{128, t_128};
+}
+
+bool small_tiles(const GemmFp8Args &a, const TilePlan &t, const PairPlan &p, const Device &d) {
+    if (a.M <= 64) return true;
+    const int64_t ctas = t.tiles * t.splits, each = (t.groups + t.splits - 1) / t.splits;
+    const int64_t rounds = (t.tiles + d.clusters[t.tile_m <= 64][31 - __builtin_clz((unsigned)t.splits)] - 1) /
+                           d.clusters[t.tile_m <= 64][31 - __builtin_clz((unsigned)t.splits)];
+    return 570 + (t.splits < 8 ? 100 : 0) + rounds * each * (ctas <= d.sms ? 30 : 50) < p.time;
 }
 
 }  // namespace
@@ -819,8 +849,13 @@ int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
     Device d;
     const int rc = device(&d);
     if (rc) return rc;
-    if (a.M > 256 && a.N > 256) return pair_dispatch(a, d.sms, s);
-    return tile_launch(a, d, s);
+    const TilePlan t = plan_tile(a, d);
+    const PairPlan p = plan_pair(a, d);
+    if (small_tiles(a, t, p, d)) return tile_launch(a, t, s);
+    const int clusters = d.sms / 2;
+    if (a.out == SVDCACHE_FP8) return p.bn == 256 ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
+    if (a.out == SVDCACHE_BF16) return p.bn == 192 ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
+    return p.bn == 192 ? pair_launch<SVDCACHE_F32, 192>(a, clusters, s) : pair_launch<SVDCACHE_F32, 128>(a, clusters, s);
 }
 
 }  // namespace svdc
