@@ -423,9 +423,7 @@ def svdcache_left_factors(C: torch.Tensor, sigma: torch.Tensor, stream=None) -> 
 # ------------------------------------------------------------- 8-bit linear path ---
 
 ACT_NONE, ACT_GELU = 0, 1
-_BYTES = (torch.uint8, torch.float8_e4m3fn)
-_SCALES = (torch.uint8, torch.float8_e8m0fnu)
-_gemm_status = {}   # device index -> the device's status word
+_gemm_status = {}   # device index -> (the device's status word, its address)
 # The current stream's handle without building a torch.cuda.Stream around it (0.1 us instead of 3.4): these calls can
 # be shorter than that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -437,47 +435,47 @@ def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
     return out.value
 
 
-def _matrix(t: torch.Tensor, what: str):
-    """(pointer, row pitch in elements) of a device matrix whose rows are contiguous."""
-    stride = t.stride()
-    if len(stride) != 2 or not t.is_cuda or stride[1] != 1:
-        if t.dim() != 2 or not t.is_cuda or t.shape[1] != 1:
-            raise ValueError(f"{what}: a device matrix with contiguous rows is expected")
-    if t.shape[0] == 1:   # torch gives a single row any stride
-        return t.data_ptr(), -(-t.shape[1] // 16) * 16
-    return t.data_ptr(), stride[0]
+# The calls below can be shorter on the GPU than a careful binding is on the host: every attribute of a tensor costs
+# 0.05-0.2 us, a nested call 0.1 us.  Hence the flat checks, each attribute read once.
+
+def _bad(what: str):
+    raise ValueError(what)
 
 
-def _fp8_matrix(q: torch.Tensor, s: torch.Tensor, rows: int, cols: int, what: str):
+def _pitch(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
+    """Row pitch, in elements, of a matrix whose rows must be contiguous; torch gives a single row any stride."""
+    ld, step = t.stride()
+    if step != 1 and cols != 1:
+        _bad(f"{what}: contiguous rows are expected")
+    return ld if rows != 1 else -(-cols // 16) * 16
+
+
+def _fp8_matrix(q: torch.Tensor, s: torch.Tensor, rows: int, cols: int, dev: int, what: str):
     """(pointer of the bytes, pitch, pointer of the scales) of an 8-bit matrix."""
-    shape = q.shape
-    if shape[0] != rows or shape[1] < cols or q.dtype not in _BYTES:
-        raise ValueError(f"{what}: {rows} x {cols} bytes are expected")
-    if s.nbytes < (rows + 127) // 128 * ((cols + 511) // 512) * 512 or s.dtype not in _SCALES or not s.is_cuda or not s.is_contiguous():
-        raise ValueError(f"{what}: a scale buffer of svdcache_fp8_scale_bytes({rows}, {cols}) bytes is expected")
-    return *_matrix(q, what), s.data_ptr()
+    r, c = q.shape
+    if r != rows or c < cols or q.itemsize != 1 or q.get_device() != dev:
+        _bad(f"{what}: {rows} x {cols} bytes on the device are expected")
+    if s.itemsize != 1 or s.numel() < (rows + 127) // 128 * ((cols + 511) // 512) * 512 or s.get_device() != dev or not s.is_contiguous():
+        _bad(f"{what}: a scale buffer of svdcache_fp8_scale_bytes({rows}, {cols}) bytes is expected")
+    return q.data_ptr(), _pitch(q, rows, c, what), s.data_ptr()
 
 
-def _vector(t: Optional[torch.Tensor], n: int, what: str):
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: {n} fp32 values on the device are expected")
+def _vector(t: torch.Tensor, n: int, dev: int, what: str):
+    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
+        _bad(f"{what}: {n} fp32 values on the device are expected")
     return t.data_ptr()
-
-
-def _stream_of(t: torch.Tensor, stream):
-    """The stream to launch on: the given one, or the current one of the tensor's device."""
-    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def svdcache_quantize_fp8(X: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, tile_rows: int = 1, stream=None) -> None:
     """X [rows, cols] fp32 or bf16 -> e4m3 bytes Q [rows, >= cols] and their scales S (see new_fp8); one scale per
     1 x 128 group, or with tile_rows = 128 per 128 x 128 tile."""
-    x, ld = _matrix(X, "X")
     rows, cols = X.shape
-    q, ldq, s = _fp8_matrix(Q, S, rows, cols, "Q")
-    rc = (_lib or lib()).svdcache_quantize_fp8(x, rows, cols, ld, _DTYPES[X.dtype], tile_rows, q, ldq, s, _stream_of(X, stream))
+    dev = X.get_device()
+    if dev < 0:
+        _bad("X: a device matrix is expected")
+    q, ldq, s = _fp8_matrix(Q, S, rows, cols, dev, "Q")
+    rc = (_lib or lib()).svdcache_quantize_fp8(X.data_ptr(), rows, cols, _pitch(X, rows, cols, "X"), _DTYPES[X.dtype], tile_rows, q, ldq, s,
+                                               _raw_stream(dev) if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "quantize_fp8")
 
@@ -487,22 +485,24 @@ def svdcache_residual_rmsnorm_fp8(H: torch.Tensor, X: Optional[torch.Tensor], H_
                                   stream=None) -> None:
     """h = H + X (X None: h = H) -> H_out (None: not kept; H itself: in place); RMS norm of h times weight [D] fp32
     (None: ones) as an 8-bit matrix Q, S."""
-    h, ldh = _matrix(H, "H")
-    shape, dtype = H.shape, H.dtype
+    shape, dtype, dev = H.shape, H.dtype, H.get_device()
     rows, D = shape
+    if dev < 0:
+        _bad("H: a device matrix is expected")
     x = o = None
     ldx = ldo = 0
     if X is not None:
-        if X.shape != shape or X.dtype != dtype:
-            raise ValueError("X: H's shape and type are expected")
-        x, ldx = _matrix(X, "X")
+        if X.shape != shape or X.dtype is not dtype or X.get_device() != dev:
+            _bad("X: H's shape, type and device are expected")
+        x, ldx = X.data_ptr(), _pitch(X, rows, D, "X")
     if H_out is not None:
-        if H_out.shape != shape or H_out.dtype != dtype:
-            raise ValueError("H_out: H's shape and type are expected")
-        o, ldo = _matrix(H_out, "H_out")
-    q, ldq, s = _fp8_matrix(Q, S, rows, D, "Q")
-    rc = (_lib or lib()).svdcache_residual_rmsnorm_fp8(h, ldh, x, ldx, o, ldo, _vector(weight, D, "weight"), eps, q, ldq, s, rows, D,
-                                                       _DTYPES[dtype], _stream_of(H, stream))
+        if H_out.shape != shape or H_out.dtype is not dtype or H_out.get_device() != dev:
+            _bad("H_out: H's shape, type and device are expected")
+        o, ldo = H_out.data_ptr(), _pitch(H_out, rows, D, "H_out")
+    q, ldq, s = _fp8_matrix(Q, S, rows, D, dev, "Q")
+    rc = (_lib or lib()).svdcache_residual_rmsnorm_fp8(
+        H.data_ptr(), _pitch(H, rows, D, "H"), x, ldx, o, ldo, None if weight is None else _vector(weight, D, dev, "weight"), eps, q, ldq, s,
+        rows, D, _DTYPES[dtype], _raw_stream(dev) if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "residual_rmsnorm_fp8")
 
@@ -514,24 +514,30 @@ def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: to
     (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
     one per device, which gemm_status() reads."""
     M, N = C.shape
-    a, lda, sa = _fp8_matrix(A, SA, M, K, "A")
-    b, ldb, sb = _fp8_matrix(B, SB, N, K, "B")
-    dtype = C.dtype
-    if dtype in _BYTES:
+    dev = C.get_device()
+    if dev < 0:
+        _bad("C: a device matrix is expected")
+    a, lda, sa = _fp8_matrix(A, SA, M, K, dev, "A")
+    b, ldb, sb = _fp8_matrix(B, SB, N, K, dev, "B")
+    if C.itemsize == 1:
         if S_out is None:
-            raise ValueError("S_out: an 8-bit C needs a scale buffer")
+            _bad("S_out: an 8-bit C needs a scale buffer")
         out = FP8
-        c, ldc, sc = _fp8_matrix(C, S_out, M, N, "C")
+        c, ldc, sc = _fp8_matrix(C, S_out, M, N, dev, "C")
     else:
-        out, sc = _DTYPES[dtype], None
-        c, ldc = _matrix(C, "C")
+        out, sc = _DTYPES[C.dtype], None
+        c, ldc = C.data_ptr(), _pitch(C, M, N, "C")
     if status is None:
-        status = _gemm_status.get(C.get_device())
-        if status is None:
-            status = _gemm_status[C.get_device()] = torch.zeros(1, dtype=torch.int32, device=C.device)
-            torch.cuda.synchronize(C.device)   # the zero is there whatever stream the product runs on
-    rc = (_lib or lib()).svdcache_gemm_fp8(a, lda, sa, b, ldb, sb, _vector(bias, N, "bias"), act, c, ldc, out, sc, M, N, K,
-                                           status.data_ptr(), _stream_of(C, stream))
+        word = _gemm_status.get(dev)
+        if word is None:
+            status = torch.zeros(1, dtype=torch.int32, device=C.device)
+            torch.cuda.synchronize(dev)   # the zero is there whatever stream the product runs on
+            word = (_gemm_status.setdefault(dev, (status, status.data_ptr())))
+        word = word[1]
+    else:
+        word = status.data_ptr()
+    rc = (_lib or lib()).svdcache_gemm_fp8(a, lda, sa, b, ldb, sb, None if bias is None else _vector(bias, N, dev, "bias"), act, c, ldc, out, sc,
+                                           M, N, K, word, _raw_stream(dev) if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "gemm_fp8")
 
@@ -542,7 +548,7 @@ def gemm_status(device="cuda") -> int:
     device = torch.device(device)
     torch.cuda.synchronize(device)
     status = _gemm_status.get(torch.cuda.current_device() if device.index is None else device.index)
-    return 0 if status is None else int(status.item())
+    return 0 if status is None else int(status[0].item())
 
 
 def new_fp8(rows: int, cols: int, device="cuda"):
