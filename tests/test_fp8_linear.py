@@ -228,6 +228,14 @@ def test_product_at_the_widths_of_the_streams(out):
 
 
 @gpu
+@pytest.mark.parametrize("M,N,K", [(9200, 1400, 200), (4600, 1500, 328), (5000, 2300, 129), (20000, 300, 640)])
+def test_product_of_many_tiles_per_cluster(M, N, K):
+    """Every width of tile over several rounds, with a last column tile that ends in each part of it."""
+    run_product(M, N, K, "bf16", sc.ACT_NONE, True, seed=1)
+    run_product(M, N, K, "fp8", sc.ACT_GELU, True, seed=2)
+
+
+@gpu
 @pytest.mark.parametrize("M", [4, 700])
 def test_nan_codes_stay_in_their_row_and_column(M):
     N, K = 300, 700
