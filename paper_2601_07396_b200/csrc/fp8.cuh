@@ -59,15 +59,42 @@ __device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d
     return lo | (hi << 16);
 }
 
+// Two fp32 values in one 64-bit register, and the arithmetic that takes such pairs in one instruction.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void pair_to(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // x / (1 + exp(-2u)) by ex2 and rcp (each good to a few 2^-23): exp(-2u) = 2^(x (a + b x^2)).  Beyond the range of
 // exp the quotient is 0 or x.  The ftz forms are one instruction each; what they flush (exp below 2^-126 beside the 1, a
 // quotient below |x| 2^-126) is far below the sum's own rounding.
-__device__ __forceinline__ float gelu_tanh(float x) {
-    const float t = x * fmaf(x * x, -0.10294324f, -2.3022082f);    // -2 sqrt(2 / pi) log2(e) {0.044715, 1}
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return x * r;
+__device__ __forceinline__ uint64_t gelu_tanh(uint64_t x) {
+    constexpr float kA = -2.3022082f, kB = -0.10294324f;           // -2 sqrt(2 / pi) log2(e) {1, 0.044715}
+    float t0, t1, e0, e1;
+    pair_to(pair_mul(x, pair_fma(pair_mul(x, x), pair_of(kB, kB), pair_of(kA, kA))), t0, t1);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
+    pair_to(pair_add(pair_of(e0, e1), pair_of(1.0f, 1.0f)), e0, e1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(e0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(e1));
+    return pair_mul(x, pair_of(e0, e1));
 }
 
 // These kernels are short and follow one another, so each may be launched while the one before it still runs: what

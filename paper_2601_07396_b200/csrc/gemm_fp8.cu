@@ -89,9 +89,10 @@ __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t parts,
                 v[0] += part[i][x].x; v[1] += part[i][x].y; v[2] += part[i][x].z; v[3] += part[i][x].w;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] += bias[j];
-                if (p.act == SVDCACHE_ACT_GELU) v[j] = gelu_tanh(v[j]);
+            for (int j = 0; j < 4; ++j) v[j] += bias[j];
+            if (p.act == SVDCACHE_ACT_GELU) {
+                pair_to(gelu_tanh(pair_of(v[0], v[1])), v[0], v[1]);
+                pair_to(gelu_tanh(pair_of(v[2], v[3])), v[2], v[3]);
             }
             const int64_t m = m_first + r0 + i;
             const bool live = r0 + i < rows;
@@ -337,11 +338,12 @@ template <int N> __device__ __forceinline__ void add_bias_and_act(float *v, cons
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
         const float4 b = *reinterpret_cast<const float4 *>(bias + i);
-        v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+        pair_to(pair_add(pair_of(v[i], v[i + 1]), pair_of(b.x, b.y)), v[i], v[i + 1]);
+        pair_to(pair_add(pair_of(v[i + 2], v[i + 3]), pair_of(b.z, b.w)), v[i + 2], v[i + 3]);
     }
     if (act == SVDCACHE_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = gelu_tanh(v[i]);
+        for (int i = 0; i < N; i += 2) pair_to(gelu_tanh(pair_of(v[i], v[i + 1])), v[i], v[i + 1]);
     }
 }
 
@@ -547,7 +549,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                     }
                 }
                 const uint32_t byte = fp8_scale_byte(top);
-                const float inv = fp8_inverse_scale(byte);
+                const uint64_t inv = pair_of(fp8_inverse_scale(byte), fp8_inverse_scale(byte));
                 if (lane == 0) tma_store_wait_read<0>();      // the last box has left
                 __syncwarp();
 #pragma unroll
@@ -556,7 +558,10 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int k = c * 16 + i * 4;
-                        w[i] = fp8_pack4(v[k] * inv, v[k + 1] * inv, v[k + 2] * inv, v[k + 3] * inv);
+                        float x[4];
+                        pair_to(pair_mul(pair_of(v[k], v[k + 1]), inv), x[0], x[1]);
+                        pair_to(pair_mul(pair_of(v[k + 2], v[k + 3]), inv), x[2], x[3]);
+                        w[i] = fp8_pack4(x[0], x[1], x[2], x[3]);
                     }
                     shared_store(store_row + (uint32_t)(c ^ (lane & 7)) * 16u, w);
                 }
