@@ -314,7 +314,7 @@ template <int BN> struct Pair {
     static_assert(kStages >= 4 && (BN == 256 || 2 * BN <= (int)kScaleCol), "shared and tensor memory");
 };
 // Tiles are walked in bands of at most this many tile rows, column by column: the clusters at work share a few columns
-// of B's tiles and the band's rows of A.  (4608 x 12288 x 3072: 135 us with bands of 8, 129 with one of 18; 118800 x 3072
+// of B's tiles and the band's rows of A.  (4608 x 12288 x 3072 into bf16: 134 us with bands of 8, 130 with one of 18; into
 // 8 bits with gelu 138 and 136.)
 constexpr int kBandRows = 20;
 
@@ -497,19 +497,25 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         const uint32_t acc_empty_first = cluster_addr(acc_empty + (kHalves ? 0 : 8 * group), 0);
         constexpr int kCols = OUT == SVDCACHE_FP8 ? 128 : OUT == SVDCACHE_BF16 ? 64 : 32;   // columns of C in 128 bytes
         constexpr int kBlocks = T::kWarpCols / 32;                                          // column blocks of a tensor-memory load
+        float next_bias[kBlocks];
+        auto request_bias = [&](int t) {
+            const int n0 = t < p.tiles ? pair_tile(p, t).n * BN + (kHalves ? group * 128 : 0) + lane : p.N;
+#pragma unroll
+            for (int j = 0; j < kBlocks; ++j) next_bias[j] = p.bias && n0 + j * 32 < p.N ? __ldg(p.bias + n0 + j * 32) : 0.0f;
+        };
+        request_bias(cluster + (kHalves ? 0 : group * clusters));
         uint32_t it = 0;
         for (int t = cluster; t < p.tiles; t += clusters, ++it) {
             if (!kHalves && (int)(it & 1u) != group) continue;
             const TileAt at = pair_tile(p, t);
             const int64_t row0 = (int64_t)at.m * kPairM + rank * 128 + q * 32;
             const int col0 = at.n * BN + (kHalves ? group * 128 : 0);
+            // this tile's bias was requested a tile ago
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < kBlocks; ++j) {
-                const int n = col0 + j * 32 + lane;
-                bias[j * 32 + lane] = p.bias && n < p.N ? p.bias[n] : 0.0f;
-            }
+            for (int j = 0; j < kBlocks; ++j) bias[j * 32 + lane] = next_bias[j];
             __syncwarp();
+            request_bias(t + (kHalves ? 1 : 2) * clusters);
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full + (kHalves ? 0 : 8 * group), (kHalves ? it : it >> 1) & 1u, abort_flag, 4))) goto done;
             tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (it & 1u) * T::kAccStep + (kHalves ? group * 128 : 0);
@@ -568,8 +574,8 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                     }
                     shared_store(store_row + (uint32_t)(c ^ (lane & 7)) * 16u, w);
                 }
+                send_box<uint8_t>(&tm_c, p, store, col0, row0, lane);   // its fence waits for earlier stores: the scale's comes after
                 if (row0 + lane < p.M && col0 < p.N) p.SC[fp8_scale_offset(row0 + lane, col0 / kFp8Group, p.pieces_c)] = (uint8_t)byte;
-                send_box<uint8_t>(&tm_c, p, store, col0, row0, lane);
             } else {
 #pragma unroll 1
                 for (int j = 0; j < kBlocks; ++j) {
