@@ -1,11 +1,14 @@
 """Thin ctypes binding of ``libsvdcache.so``: same names as ``include/svdcache.h``,
-argument marshalling only (tensor -> raw pointer, current stream -> void*).  Every step
+argument marshalling only (tensor -> raw pointer, current stream -> void*; for the 8-bit calls
+by the extension ``_calls.so``).  Every step
 of the path runs in the library's CUDA kernels; nothing here computes, and there is no
 fallback: a missing library or a failing call raises.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 from typing import Optional, Tuple
 
@@ -423,10 +426,8 @@ def svdcache_left_factors(C: torch.Tensor, sigma: torch.Tensor, stream=None) -> 
 # ------------------------------------------------------------- 8-bit linear path ---
 
 ACT_NONE, ACT_GELU = 0, 1
-_gemm_status = {}   # device index -> (the device's status word, its address)
-# The current stream's handle without building a torch.cuda.Stream around it (0.1 us instead of 3.4): these calls can
-# be shorter than that.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_gemm_status = {}    # device index -> address of the device's status word
+_status_words = []
 
 
 def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
@@ -435,47 +436,32 @@ def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
     return out.value
 
 
-# The calls below can be shorter on the GPU than a careful binding is on the host: every attribute of a tensor costs
-# 0.05-0.2 us, a nested call 0.1 us.  Hence the flat checks, each attribute read once.
-
-def _bad(what: str):
-    raise ValueError(what)
-
-
-def _pitch(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
-    """Row pitch, in elements, of a matrix whose rows must be contiguous; torch gives a single row any stride."""
-    ld, step = t.stride()
-    if step != 1 and cols != 1:
-        _bad(f"{what}: contiguous rows are expected")
-    return ld if rows != 1 else -(-cols // 16) * 16
+# The calls below can be shorter on the GPU than a binding in Python is on the host, so their arguments are read and
+# checked by a small extension (csrc/calls.cpp), which calls the same C entry points.  It raises ValueError for
+# arguments that the C ABI cannot see to be wrong (shapes against one another, device, contiguity).
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
+_calls = None
 
 
-def _fp8_matrix(q: torch.Tensor, s: torch.Tensor, rows: int, cols: int, dev: int, what: str):
-    """(pointer of the bytes, pitch, pointer of the scales) of an 8-bit matrix."""
-    r, c = q.shape
-    if r != rows or c < cols or q.itemsize != 1 or q.get_device() != dev:
-        _bad(f"{what}: {rows} x {cols} bytes on the device are expected")
-    if s.itemsize != 1 or s.numel() < (rows + 127) // 128 * ((cols + 511) // 512) * 512 or s.get_device() != dev or not s.is_contiguous():
-        _bad(f"{what}: a scale buffer of svdcache_fp8_scale_bytes({rows}, {cols}) bytes is expected")
-    return q.data_ptr(), _pitch(q, rows, c, what), s.data_ptr()
-
-
-def _vector(t: torch.Tensor, n: int, dev: int, what: str):
-    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
-        _bad(f"{what}: {n} fp32 values on the device are expected")
-    return t.data_ptr()
+def calls():
+    """Load the extension (once) and bind it to the library.  Raises if it has not been built."""
+    global _calls
+    if _calls is None:
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError(f"{CALLS_PATH} is missing: build it with `python -m paper_2601_07396_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_calls", CALLS_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+        loader.exec_module(module)
+        L = lib()
+        module.bind(*[ctypes.cast(f, _vp).value for f in (L.svdcache_quantize_fp8, L.svdcache_residual_rmsnorm_fp8, L.svdcache_gemm_fp8)])
+        _calls = module
+    return _calls
 
 
 def svdcache_quantize_fp8(X: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, tile_rows: int = 1, stream=None) -> None:
     """X [rows, cols] fp32 or bf16 -> e4m3 bytes Q [rows, >= cols] and their scales S (see new_fp8); one scale per
     1 x 128 group, or with tile_rows = 128 per 128 x 128 tile."""
-    rows, cols = X.shape
-    dev = X.get_device()
-    if dev < 0:
-        _bad("X: a device matrix is expected")
-    q, ldq, s = _fp8_matrix(Q, S, rows, cols, dev, "Q")
-    rc = (_lib or lib()).svdcache_quantize_fp8(X.data_ptr(), rows, cols, _pitch(X, rows, cols, "X"), _DTYPES[X.dtype], tile_rows, q, ldq, s,
-                                               _raw_stream(dev) if stream is None else stream.cuda_stream)
+    rc = (_calls or calls()).quantize(X, Q, S, tile_rows, None if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "quantize_fp8")
 
@@ -485,24 +471,7 @@ def svdcache_residual_rmsnorm_fp8(H: torch.Tensor, X: Optional[torch.Tensor], H_
                                   stream=None) -> None:
     """h = H + X (X None: h = H) -> H_out (None: not kept; H itself: in place); RMS norm of h times weight [D] fp32
     (None: ones) as an 8-bit matrix Q, S."""
-    shape, dtype, dev = H.shape, H.dtype, H.get_device()
-    rows, D = shape
-    if dev < 0:
-        _bad("H: a device matrix is expected")
-    x = o = None
-    ldx = ldo = 0
-    if X is not None:
-        if X.shape != shape or X.dtype is not dtype or X.get_device() != dev:
-            _bad("X: H's shape, type and device are expected")
-        x, ldx = X.data_ptr(), _pitch(X, rows, D, "X")
-    if H_out is not None:
-        if H_out.shape != shape or H_out.dtype is not dtype or H_out.get_device() != dev:
-            _bad("H_out: H's shape, type and device are expected")
-        o, ldo = H_out.data_ptr(), _pitch(H_out, rows, D, "H_out")
-    q, ldq, s = _fp8_matrix(Q, S, rows, D, dev, "Q")
-    rc = (_lib or lib()).svdcache_residual_rmsnorm_fp8(
-        H.data_ptr(), _pitch(H, rows, D, "H"), x, ldx, o, ldo, None if weight is None else _vector(weight, D, dev, "weight"), eps, q, ldq, s,
-        rows, D, _DTYPES[dtype], _raw_stream(dev) if stream is None else stream.cuda_stream)
+    rc = (_calls or calls()).norm(H, X, H_out, weight, eps, Q, S, None if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "residual_rmsnorm_fp8")
 
@@ -513,33 +482,20 @@ def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: to
     """C [M, N] = act(A B^T + bias) of the 8-bit matrices A [M, >= K] and B [N, >= K].  C is fp32 or bf16, or bytes
     (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
     one per device, which gemm_status() reads."""
-    M, N = C.shape
-    dev = C.get_device()
-    if dev < 0:
-        _bad("C: a device matrix is expected")
-    a, lda, sa = _fp8_matrix(A, SA, M, K, dev, "A")
-    b, ldb, sb = _fp8_matrix(B, SB, N, K, dev, "B")
-    if C.itemsize == 1:
-        if S_out is None:
-            _bad("S_out: an 8-bit C needs a scale buffer")
-        out = FP8
-        c, ldc, sc = _fp8_matrix(C, S_out, M, N, dev, "C")
-    else:
-        out, sc = _DTYPES[C.dtype], None
-        c, ldc = C.data_ptr(), _pitch(C, M, N, "C")
-    if status is None:
-        word = _gemm_status.get(dev)
-        if word is None:
-            status = torch.zeros(1, dtype=torch.int32, device=C.device)
-            torch.cuda.synchronize(dev)   # the zero is there whatever stream the product runs on
-            word = (_gemm_status.setdefault(dev, (status, status.data_ptr())))
-        word = word[1]
-    else:
-        word = status.data_ptr()
-    rc = (_lib or lib()).svdcache_gemm_fp8(a, lda, sa, b, ldb, sb, None if bias is None else _vector(bias, N, dev, "bias"), act, c, ldc, out, sc,
-                                           M, N, K, word, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    word = status.data_ptr() if status is not None else _gemm_status.get(C.get_device()) or _new_status(C)
+    rc = (_calls or calls()).gemm(A, SA, B, SB, K, C, S_out, bias, act, word, None if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "gemm_fp8")
+
+
+def _new_status(C: torch.Tensor) -> int:
+    """A zeroed status word for C's device, kept until the process ends; its address."""
+    if not C.is_cuda:
+        raise ValueError("C: a device matrix is expected")
+    word = torch.zeros(1, dtype=torch.int32, device=C.device)
+    torch.cuda.synchronize(C.device)   # the zero is there whatever stream the product runs on
+    _status_words.append(word)
+    return _gemm_status.setdefault(C.get_device(), word.data_ptr())
 
 
 def gemm_status(device="cuda") -> int:
@@ -547,8 +503,8 @@ def gemm_status(device="cuda") -> int:
     bounded wait ran out in one of them."""
     device = torch.device(device)
     torch.cuda.synchronize(device)
-    status = _gemm_status.get(torch.cuda.current_device() if device.index is None else device.index)
-    return 0 if status is None else int(status[0].item())
+    address = _gemm_status.get(torch.cuda.current_device() if device.index is None else device.index)
+    return next((int(w.item()) for w in _status_words if w.data_ptr() == address), 0)
 
 
 def new_fp8(rows: int, cols: int, device="cuda"):

@@ -1,14 +1,18 @@
-"""Builds ``libsvdcache.so`` (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds ``libsvdcache.so`` (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and ``_calls.so`` (the argument side
+of the 8-bit calls, a Python extension over torch's tensors) with the host compiler."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsvdcache.so")
+CALLS_SOURCE = os.path.join(CSRC, "calls.cpp")
+CALLS = os.path.join(HERE, "_calls.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -29,8 +33,27 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_calls(force: bool = False) -> str:
+    """Compile csrc/calls.cpp into the extension.  Returns its path."""
+    deps = [CALLS_SOURCE, os.path.join(HERE, "..", "include", "svdcache.h")]
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(d) <= os.path.getmtime(CALLS) for d in deps):
+        return CALLS
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [sysconfig.get_paths()["include"], *cpp_extension.include_paths(), os.path.join(cuda, "include")]
+    lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = CALLS + f".tmp{os.getpid()}"
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for d in include for a in ("-isystem", d)],
+                    CALLS_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared object.  Returns its path."""
+    """Compile every .cu under csrc/ into one shared object, and the extension.  Returns the library's path."""
+    build_calls(force)
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
