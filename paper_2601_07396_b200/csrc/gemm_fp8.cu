@@ -13,6 +13,7 @@
 // its mbarrier), and finishes its own share, adding the parts in rank order: no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
 #include <atomic>
+#include <cstring>
 #include <type_traits>
 
 #include "fp8.cuh"
@@ -351,11 +352,11 @@ template <int N> __device__ __forceinline__ void add_bias_and_act(float *v, cons
 }
 
 // A warp's box of C (32 rows of 128 bytes, 16-byte pieces swizzled), written by all its lanes, on its way out.  A TMA
-// store ends at a multiple of 16 bytes, not at the matrix's last column: a box that the last column cuts elsewhere is
-// written by the lanes, so that nothing beyond column N changes.
+// store ends at a multiple of 16 bytes, not at the matrix's last column: of a box that the last column cuts elsewhere
+// each lane writes a row, so that nothing beyond column N changes.
 template <typename T>
 __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairParams &p, uint32_t box, int n, int64_t row0, int lane) {
-    constexpr int kCols = 128 / (int)sizeof(T);
+    constexpr int kCols = 128 / (int)sizeof(T), kPiece = 16 / (int)sizeof(T);
     if (n >= p.N || row0 >= p.M) return;
     if (n + kCols <= p.N || (p.N * (int)sizeof(T)) % 16 == 0) {
         fence_proxy_async();
@@ -366,15 +367,22 @@ __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairPara
         }
         return;
     }
-    __syncwarp();
-    for (int r = 0; r < 32 && row0 + r < p.M; ++r) {
-        T *out = reinterpret_cast<T *>(p.C) + (row0 + r) * p.ldc + n;
-        for (int c = lane; c < p.N - n; c += 32) {
-            const uint32_t byte = (uint32_t)c * sizeof(T);
-            const uint32_t at = box + (uint32_t)r * 128u + ((byte >> 4) ^ (uint32_t)(r & 7)) * 16u + (byte & 15u);
-            if constexpr (sizeof(T) == 4) asm volatile("{.reg .b32 v; ld.shared.b32 v, [%1]; st.global.b32 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
-            else if constexpr (sizeof(T) == 2) asm volatile("{.reg .b16 v; ld.shared.b16 v, [%1]; st.global.b16 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
-            else asm volatile("{.reg .b16 v; ld.shared.b8 v, [%1]; st.global.b8 [%0], v;}" ::"l"(out + c), "r"(at) : "memory");
+    if (row0 + lane < p.M) {
+        T *out = reinterpret_cast<T *>(p.C) + (row0 + lane) * p.ldc + n;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int left = p.N - n - c * kPiece;       // columns from this piece on
+            if (left <= 0) break;
+            const float4 f = shared_load(box + (uint32_t)lane * 128u + (uint32_t)(c ^ (lane & 7)) * 16u);
+            T v[kPiece];
+            memcpy(v, &f, 16);
+            if (left >= kPiece) {
+                *reinterpret_cast<float4 *>(out + c * kPiece) = f;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i)
+                    if (i < left) out[c * kPiece + i] = v[i];
+            }
         }
     }
     __syncwarp();
