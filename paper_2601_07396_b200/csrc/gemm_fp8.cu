@@ -314,10 +314,12 @@ template <int BN> struct Pair {
     static constexpr int kWarpCols = kHalves ? 128 : BN;                          // columns of a tile that a warp finishes
     static_assert(kStages >= 4 && (BN == 256 || 2 * BN <= (int)kScaleCol), "shared and tensor memory");
 };
-// Tiles are walked in bands of at most this many tile rows, column by column: the clusters at work share a few columns
-// of B's tiles and the band's rows of A.  (4608 x 12288 x 3072 into bf16: 134 us with bands of 8, 130 with one of 18; into
-// 8 bits with gelu 138 and 136.)
+// Tiles are walked in bands of tile rows, column by column: the clusters at work share a few columns of B's tiles and the
+// band's rows of A.  High bands read B fewer times (4608 x 12288 x 3072 into bf16: 134 us with bands of 8 rows, 130 with
+// one of 18; into 8 bits with gelu 138 and 136), up to where a band's A no longer stays in L2 (4608 x 3072 x 12288: 128 us
+// with 57 MB in one band, 123 with bands of 25 or 31 MB).
 constexpr int kBandRows = 20;
+constexpr int64_t kBandBytes = 32 << 20;
 
 struct PairParams {
     int64_t M, ldc;
@@ -823,7 +825,8 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
     if (m_tiles * p.n_tiles > 0x3FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.m_tiles = (int)m_tiles;
     p.tiles = p.m_tiles * p.n_tiles;
-    const int bands = (p.m_tiles + kBandRows - 1) / kBandRows;
+    const int64_t fit = kBandBytes / ((int64_t)kPairM * a.K), most = fit < 4 ? 4 : fit > kBandRows ? kBandRows : fit;
+    const int bands = (int)((p.m_tiles + most - 1) / most);
     p.band_rows = (p.m_tiles + bands - 1) / bands;
     p.bias = a.bias; p.SC = (uint8_t *)a.SC; p.pieces_c = fp8_piece_cols(a.N); p.act = a.act; p.status = a.status;
     CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_c;
