@@ -359,35 +359,35 @@ template <int N> __device__ __forceinline__ void add_bias_and_act(float *v, cons
 template <typename T>
 __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairParams &p, uint32_t box, int n, int64_t row0, int lane) {
     constexpr int kCols = 128 / (int)sizeof(T), kPiece = 16 / (int)sizeof(T);
-    if (n >= p.N || row0 >= p.M) return;
-    if (n + kCols <= p.N || (p.N * (int)sizeof(T)) % 16 == 0) {
+    const bool live = n < p.N && row0 < p.M, whole = n + kCols <= p.N || (p.N * (int)sizeof(T)) % 16 == 0;
+    if (live && whole) {
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
             tma_store_2d(tm_c, box, n, (int)row0);
             tma_store_commit();
         }
-        return;
-    }
-    if (row0 + lane < p.M) {
-        T *out = reinterpret_cast<T *>(p.C) + (row0 + lane) * p.ldc + n;
+    } else if (live) {
+        if (row0 + lane < p.M) {
+            T *out = reinterpret_cast<T *>(p.C) + (row0 + lane) * p.ldc + n;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const int left = p.N - n - c * kPiece;       // columns from this piece on
-            if (left <= 0) break;
-            const float4 f = shared_load(box + (uint32_t)lane * 128u + (uint32_t)(c ^ (lane & 7)) * 16u);
-            T v[kPiece];
-            memcpy(v, &f, 16);
-            if (left >= kPiece) {
-                *reinterpret_cast<float4 *>(out + c * kPiece) = f;
-            } else {
+            for (int c = 0; c < 8; ++c) {
+                const int left = p.N - n - c * kPiece;       // columns from this piece on
+                if (left <= 0) break;
+                const float4 f = shared_load(box + (uint32_t)lane * 128u + (uint32_t)(c ^ (lane & 7)) * 16u);
+                T v[kPiece];
+                memcpy(v, &f, 16);
+                if (left >= kPiece) {
+                    *reinterpret_cast<float4 *>(out + c * kPiece) = f;
+                } else {
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i)
-                    if (i < left) out[c * kPiece + i] = v[i];
+                    for (int i = 0; i < kPiece; ++i)
+                        if (i < left) out[c * kPiece + i] = v[i];
+                }
             }
         }
+        __syncwarp();
     }
-    __syncwarp();
 }
 
 template <int OUT, int BN>
@@ -505,7 +505,6 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         const uint32_t store_row = store + (uint32_t)lane * 128u;
         float *bias = bias_mem[warp - 2];
         const uint32_t acc_empty_first = cluster_addr(acc_empty + (kHalves ? 0 : 8 * group), 0);
-        constexpr int kCols = OUT == SVDCACHE_FP8 ? 128 : OUT == SVDCACHE_BF16 ? 64 : 32;   // columns of C in 128 bytes
         constexpr int kBlocks = T::kWarpCols / 32;                                          // column blocks of a tensor-memory load
         float next_bias[kBlocks];
         auto request_bias = [&](int t) {
@@ -587,22 +586,20 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 send_box<uint8_t>(&tm_c, p, store, col0, row0, lane);   // its fence waits for earlier stores: the scale's comes after
                 if (row0 + lane < p.M && col0 < p.N) p.SC[fp8_scale_offset(row0 + lane, col0 / kFp8Group, p.pieces_c)] = (uint8_t)byte;
             } else {
-#pragma unroll 1
-                for (int j = 0; j < kBlocks; ++j) {
-                    uint32_t r[32];
-                    tmem_ld_32x32(acc + j * 32, r);
-                    tmem_wait_ld();
-                    if (j == kBlocks - 1) release();
+                // a block of 32 columns at a time, the next one on its way from tensor memory meanwhile; a box holds two
+                // blocks of bf16 (128 bytes of a row: 64 were 5-13 % slower where C's bytes count) or one of fp32
+                using C = typename std::conditional<OUT == SVDCACHE_BF16, __nv_bfloat16, float>::type;
+                constexpr int kPerBox = OUT == SVDCACHE_BF16 ? 2 : 1;
+                auto finish = [&](const uint32_t (&r)[32], int j, bool second) {
                     float v[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
                     add_bias_and_act<32>(v, bias + j * 32, p.act);
-                    constexpr int kPerBox = kCols / 32;       // blocks per box
-                    if (j % kPerBox == 0) {
-                        if (lane == 0) tma_store_wait_read<0>();
+                    if (kPerBox == 1 || !second) {
+                        if (lane == 0) tma_store_wait_read<0>();      // the last box has left
                         __syncwarp();
                     }
-                    const int c0 = j % kPerBox * 4;
+                    const uint32_t c0 = kPerBox == 2 && second ? 4u : 0u;
 #pragma unroll
                     for (int c = 0; c < 8 / kPerBox; ++c) {
                         uint32_t w[4];
@@ -615,11 +612,21 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                                 w[i] = __float_as_uint(v[c * 4 + i]);
                             }
                         }
-                        shared_store(store_row + (uint32_t)((c0 + c) ^ (lane & 7)) * 16u, w);
+                        shared_store(store_row + ((c0 + c) ^ (uint32_t)(lane & 7)) * 16u, w);
                     }
-                    if (j % kPerBox == kPerBox - 1)
-                        send_box<typename std::conditional<OUT == SVDCACHE_BF16, __nv_bfloat16, float>::type>(
-                            &tm_c, p, store, col0 + j / kPerBox * kCols, row0, lane);
+                    if (kPerBox == 1 || second) send_box<C>(&tm_c, p, store, col0 + (j - (kPerBox - 1)) * 32, row0, lane);
+                };
+                uint32_t even[32], odd[32];
+                tmem_ld_32x32(acc, even);
+#pragma unroll 1
+                for (int j = 0; j < kBlocks; j += 2) {
+                    tmem_wait_ld();
+                    tmem_ld_32x32(acc + (j + 1) * 32, odd);
+                    finish(even, j, false);
+                    tmem_wait_ld();
+                    if (j + 2 < kBlocks) tmem_ld_32x32(acc + (j + 2) * 32, even);
+                    else release();
+                    finish(odd, j + 1, true);
                 }
             }
         }
@@ -812,8 +819,8 @@ int out_map(CUtensorMap *m, const GemmFp8Args &a) {
     const cuuint64_t strides[1] = {(cuuint64_t)a.ldc * elem};
     const cuuint32_t box[2] = {(cuuint32_t)(128 / elem), 32};
     const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(m, t, 2, a.C, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUresult r = fn(m, t, 2, a.C, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
