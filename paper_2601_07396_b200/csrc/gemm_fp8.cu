@@ -534,7 +534,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             auto release = [&] {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(acc_empty_first);
+                if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_first);
             };
             if (kHalves && !shares) release();
             if constexpr (OUT == SVDCACHE_FP8) {

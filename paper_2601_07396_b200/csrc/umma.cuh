@@ -185,9 +185,15 @@ __device__ __forceinline__ void shared_store(uint32_t addr, const uint32_t (&w)[
 __device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
-// arrival on an mbarrier of another CTA of the cluster (an address from cluster_addr)
+// arrival on an mbarrier of another CTA of the cluster (an address from cluster_addr), after this thread's memory
+// operations
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// The same where there is no memory to publish, only tensor memory that has been read (tcgen05.wait::ld and
+// tc_fence_before() come before it): without the release, which waits 2000-3500 cycles for the stores under way.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Bounded wait for arrivals from the whole cluster and the shared-memory stores before them.  It does not give up when
 // another thread has: whoever else holds this CTA's addresses must be done with them before the CTA leaves.
