@@ -321,10 +321,24 @@ template <int BN> struct Pair {
 constexpr int kBandRows = 20;
 constexpr int64_t kBandBytes = 32 << 20;
 
+// Quotients by a divisor that the host knows, without the device's division (three of which a tile cost 400 cycles):
+// with 2^l the least power of two >= d and m = 2^32 (2^l - d) / d + 1, n / d = (umulhi(m, n) + n) >> l (Granlund and
+// Montgomery), for 0 <= n < 2^31.
+struct Divisor {
+    uint32_t d, m, l;
+    __host__ static Divisor of(int d) {
+        uint32_t l = 0;
+        while ((1u << l) < (uint32_t)d) ++l;
+        return {(uint32_t)d, (uint32_t)((((1ull << l) - (uint64_t)d) << 32) / (uint64_t)d + 1), l};
+    }
+    __device__ __forceinline__ int quotient(int n) const { return (int)((__umulhi(m, (uint32_t)n) + (uint32_t)n) >> l); }
+};
+
 struct PairParams {
     int64_t M, ldc;
     void *C;
-    int N, groups, m_tiles, n_tiles, tiles, band_rows;
+    int N, groups, m_tiles, n_tiles, tiles, bands;
+    Divisor band_tiles, band_rows, last_rows;        // tiles of a band; tile rows of a band, of the last one
     const float *bias;
     uint8_t *SC;
     int64_t pieces_c;
@@ -334,9 +348,10 @@ struct PairParams {
 
 struct TileAt { int m, n; };
 __device__ __forceinline__ TileAt pair_tile(const PairParams &p, int t) {
-    const int band = p.band_rows * p.n_tiles, b = t / band, in = t - b * band;
-    const int rows = min(p.band_rows, p.m_tiles - b * p.band_rows);
-    return {b * p.band_rows + in % rows, in / rows};
+    const int b = p.band_tiles.quotient(t), in = t - b * (int)p.band_tiles.d;
+    const bool last = b == p.bands - 1;
+    const int n = last ? p.last_rows.quotient(in) : p.band_rows.quotient(in);
+    return {b * (int)p.band_rows.d + in - n * (int)(last ? p.last_rows.d : p.band_rows.d), n};
 }
 
 // v += bias (shared memory, the same for every lane), then the activation
@@ -834,7 +849,11 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
     p.tiles = p.m_tiles * p.n_tiles;
     const int64_t fit = kBandBytes / ((int64_t)kPairM * a.K), most = fit < 4 ? 4 : fit > kBandRows ? kBandRows : fit;
     const int bands = (int)((p.m_tiles + most - 1) / most);
-    p.band_rows = (p.m_tiles + bands - 1) / bands;
+    const int rows = (p.m_tiles + bands - 1) / bands;
+    p.bands = (p.m_tiles + rows - 1) / rows;
+    p.band_tiles = Divisor::of(rows * p.n_tiles);
+    p.band_rows = Divisor::of(rows);
+    p.last_rows = Divisor::of(p.m_tiles - (p.bands - 1) * rows);
     p.bias = a.bias; p.SC = (uint8_t *)a.SC; p.pieces_c = fp8_piece_cols(a.N); p.act = a.act; p.status = a.status;
     CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_c;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, 128);
