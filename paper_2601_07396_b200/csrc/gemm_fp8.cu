@@ -368,6 +368,16 @@ template <int N> __device__ __forceinline__ void add_bias_and_act(float *v, cons
     }
 }
 
+// the largest magnitude of a group (NaN is passed over), as eight chains
+__device__ __forceinline__ float largest_of(const float (&v)[128]) {
+    float m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = fabsf(v[i]);
+#pragma unroll
+    for (int i = 8; i < 128; ++i) m[i & 7] = fmaxf(m[i & 7], fabsf(v[i]));
+    return fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), fmaxf(fmaxf(m[4], m[5]), fmaxf(m[6], m[7])));
+}
+
 // A warp's box of C (32 rows of 128 bytes, 16-byte pieces swizzled), written by all its lanes, on its way out.  A TMA
 // store ends at a multiple of 16 bytes, not at the matrix's last column: of a box that the last column cuts elsewhere
 // each lane writes a row, so that nothing beyond column N changes.
@@ -563,7 +573,6 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 }
                 tmem_wait_ld();
                 if (!kHalves || shares) release();
-                float top = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) add_bias_and_act<32>(v + 32 * j, bias + 32 * j, p.act);
                 if (col0 + 128 > p.N) {
@@ -571,15 +580,11 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                     for (int i = 0; i < 128; ++i)
                         if (col0 + i >= p.N) v[i] = 0.0f;
                 }
-#pragma unroll
-                for (int i = 0; i < 128; ++i) top = fmaxf(top, fabsf(v[i]));
+                float top = largest_of(v);
                 if (__float_as_uint(top) == 0x7F800000u) {
-                    top = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) {
-                        v[i] = fp8_nan_if_not_finite(v[i]);
-                        top = fmaxf(top, fabsf(v[i]));
-                    }
+                    for (int i = 0; i < 128; ++i) v[i] = fp8_nan_if_not_finite(v[i]);
+                    top = largest_of(v);
                 }
                 const uint32_t byte = fp8_scale_byte(top);
                 const uint64_t inv = pair_of(fp8_inverse_scale(byte), fp8_inverse_scale(byte));
