@@ -12,6 +12,7 @@
 // every other CTA the rows of its sum that are that one's to finish (stores into its shared memory, then an arrival on
 // its mbarrier), and finishes its own share, adding the parts in rank order: no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
+#include <algorithm>
 #include <atomic>
 #include <cstring>
 #include <type_traits>
@@ -872,14 +873,15 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
                         tm_sb, tm_c, p);
 }
 
-// Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured:
-//   pairs       4.1 us from launch to end, and per round of the clusters and group of K the time of a tile's MMAs: 0.18 us at
-//               BN = 128, 0.21 at 192, 0.33 at 256 (its wait for the accumulator included)
-//   small tiles 5.7 us, 1 more where a cluster has fewer than 8 CTAs, and per group of a CTA's share of K 0.3 us, or 0.5
-//               where CTAs share SMs or their count exceeds them
-// (K = 12288, N = 1152, M = 64 / 256 / 1024: 21.9 / 22.9 / 23.2 us by pairs, 9.9 / 19.1 / 29.3 by small tiles; K = 1152,
-// N = 3072, M = 100 / 1024: 5.9 / 8.0 by pairs, 8.1 / 23.2 by small tiles.)  Up to 64 rows a pair's tile would be mostly
-// empty and its ring too short for weights from memory (1 x 18432 x 3072: 25.8 us by pairs, 13.4 by small tiles).
+// Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4096,
+// N from 128 to 18432, K from 100 to 12288; the choice is within 7 % of the better one but for a few shapes):
+//   pairs       3.1 us from launch to end, and per round of the clusters 0.4 and for a group of K 0.20 us at BN = 128, 0.23
+//               at 192, 0.35 at 256, two fifths more where rows do not begin at multiples of 128 bytes (a box's row then
+//               lies in two lines); or 4 us and B's bytes at 4 TB/s, where that is more: a pair's ring holds little of B
+//   small tiles 3.8 us up to 16 rows, else 5.7 (0.6 more for 8-bit C), and per group of a CTA's share of K 0.36 us, 0.55 at
+//               128 rows, 0.6 where two CTAs share an SM; or 4.5 us and B's bytes at 6 TB/s
+// K = 100, N = 512, M = 64: 3.9 us by pairs, 6.2 by small tiles.  K = 9000, N = 512, M = 1 / 64 / 512: 15.9 / 19.1 / 23.7
+// and 7.5 / 9.5 / 12.7.  K = 3072, N = 18432, M = 1 / 64 / 256: 24.7 / 16.2 / 18.1 and 14.0 / 15.6 / 35.0.
 struct PairPlan {
     int bn;
     int64_t time;
@@ -887,18 +889,23 @@ struct PairPlan {
 
 PairPlan plan_pair(const GemmFp8Args &a, const Device &d) {
     const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, groups = fp8_groups(a.K), clusters = d.sms / 2;
-    auto time = [&](int bn, int64_t group) { return 410 + (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters * groups * group; };
+    const int64_t fifths = (a.lda | a.ldb) % 128 ? 7 : 5;
+    auto time = [&](int bn, int64_t group) {
+        const int64_t rounds = (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters, work = rounds * (40 + groups * group * fifths / 5);
+        return std::max(310 + work, 400 + (int64_t)a.N * a.K / 40000 + work / 16);   // the last term: fewer rounds where memory decides
+    };
     const int wide = a.out == SVDCACHE_FP8 ? 256 : 192;
-    const int64_t t_wide = time(wide, wide == 256 ? 33 : 21), t_128 = time(128, 18);
+    const int64_t t_wide = time(wide, wide == 256 ? 35 : 23), t_128 = time(128, 20);
     return t_wide < t_128 ? PairPlan{wide, t_wide} : PairPlan{128, t_128};
 }
 
-bool small_tiles(const GemmFp8Args &a, const TilePlan &t, const PairPlan &p, const Device &d) {
-    if (a.M <= 64) return true;
-    const int64_t ctas = t.tiles * t.splits, each = (t.groups + t.splits - 1) / t.splits;
-    const int64_t rounds = (t.tiles + d.clusters[t.tile_m <= 64][31 - __builtin_clz((unsigned)t.splits)] - 1) /
-                           d.clusters[t.tile_m <= 64][31 - __builtin_clz((unsigned)t.splits)];
-    return 570 + (t.splits < 8 ? 100 : 0) + rounds * each * (ctas <= d.sms ? 30 : 50) < p.time;
+int64_t tile_time(const GemmFp8Args &a, const TilePlan &t, const Device &d) {
+    int log = 0;
+    while (1 << log < t.splits) ++log;
+    const int64_t fit = d.clusters[t.tile_m <= 64][log], rounds = (t.tiles + fit - 1) / fit;
+    const int64_t base = (t.tile_m == 16 ? 380 : 570) + (a.out == SVDCACHE_FP8 ? 60 : 0), each = (t.groups + t.splits - 1) / t.splits;
+    const int64_t group = t.tile_m == 128 ? 55 : t.tiles * t.splits <= d.sms ? 36 : 60;
+    return std::max(base + rounds * each * group, 450 + (int64_t)a.N * a.K / 60000);
 }
 
 }  // namespace
@@ -909,7 +916,7 @@ int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
     if (rc) return rc;
     const TilePlan t = plan_tile(a, d);
     const PairPlan p = plan_pair(a, d);
-    if (small_tiles(a, t, p, d)) return tile_launch(a, t, s);
+    if (tile_time(a, t, d) < p.time) return tile_launch(a, t, s);
     const int clusters = d.sms / 2;
     if (a.out == SVDCACHE_FP8) return p.bn == 256 ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
     if (a.out == SVDCACHE_BF16) return p.bn == 192 ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
