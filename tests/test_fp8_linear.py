@@ -317,6 +317,79 @@ def test_chain_on_another_stream_and_in_a_graph():
     assert sc.gemm_status(DEV) == 0
 
 
+@gpu
+def test_graph_with_two_branches():
+    """Two products on two streams, joined by a norm, a memset before and a copy after, captured and replayed."""
+    M, D = 300, 512
+    a, sa = random_fp8(M, D, 1, spread=0.0)
+    w = [random_fp8(D, D, 2 + i, 128, spread=0.0) for i in range(2)]
+    y = [torch.zeros(M, D, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    q, qs = sc.new_fp8(M, D)
+    h, last = torch.empty_like(y[0]), torch.empty_like(y[0])
+    side = torch.cuda.Stream()
+
+    def work():
+        y[0].zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            sc.svdcache_gemm_fp8(a, sa, *w[1], D, y[1])
+        sc.svdcache_gemm_fp8(a, sa, *w[0], D, y[0])
+        torch.cuda.current_stream().wait_stream(side)
+        sc.svdcache_residual_rmsnorm_fp8(y[0], y[1], h, None, 1e-6, q, qs)
+        last.copy_(h)
+
+    work()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (*y, h, q, qs, last)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for _ in range(3):
+        for t in (*y, h, q, qs, last):
+            t.fill_(1)
+        qs.zero_(), q.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, u) for t, u in zip((*y, h, q, qs, last), want))
+
+
+@gpu
+def test_offsets_beyond_32_bits():
+    """4.5 GB of rows: the norm in place, the quantiser, and a product with 4.5 GB of output, at rows on either side of
+    the places where a 32-bit byte or element offset would wrap, and the last ones."""
+    M, D, N = 280000, 8192, 8192
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    h = torch.randn(M, D, generator=g, device=DEV, dtype=torch.bfloat16)
+    rows = torch.tensor([0, 1, 131071, 131072, 131073, 262143, 262144, 262145, M - 2, M - 1], device=DEV)
+    before = np64(h[rows])
+    q, s = sc.new_fp8(M, D)
+    sc.svdcache_residual_rmsnorm_fp8(h, None, h, None, 1e-6, q, s)
+    np.testing.assert_array_equal(np64(h[rows]), before)
+    y = before / np.sqrt((before ** 2).mean(1, keepdims=True) + 1e-6)
+    v = unpack_rows(q, s, M, D, rows)
+    assert (np.abs(v - y) <= 2.0 ** -4 * np.abs(y) + 2.0 ** -8).all()
+    sc.svdcache_quantize_fp8(h, q, s)
+    a = unpack_rows(q, s, M, D, rows)
+    assert (np.abs(a - before) <= 2.0 ** -4 * np.abs(before) + 2.0 ** -8).all()
+    del h
+    b, sb = random_fp8(N, D, 3, 128, spread=0.0)
+    C = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    sc.svdcache_gemm_fp8(q, s, b, sb, D, C)
+    B = dequantise(b, sb, N, D)
+    want = a @ B.T
+    err = 2.0 ** -22 * (D / 32 + 10) * (np.abs(a) @ np.abs(B).T)
+    assert (np.abs(np64(C[rows]) - want) <= err + half_ulp(np.abs(want) + err, torch.bfloat16)).all()
+    assert sc.gemm_status(DEV) == 0
+
+
+def unpack_rows(q, s, M, D, rows):
+    """What the given rows of an 8-bit matrix stand for."""
+    v = q[rows, :D].view(torch.float8_e4m3fn).double()
+    e = sc.fp8_scale_exponents(s, M, D)[rows].double() - 127.0
+    return (v * torch.exp2(e).repeat_interleave(128, 1)[:, :D]).cpu().numpy()
+
+
 # ----------------------------------------------------------------------------- refusals (host only) ---
 
 INVALID, SHAPE, ALIGN = -1, -2, -3
