@@ -9,8 +9,8 @@
 // tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns are up to 128 rows of
 // C, so that few rows of C waste no tensor work.  One CTA per tile; where that leaves SMs idle, the S CTAs of a
 // cluster share a tile: CTA r takes the groups r, r + S, ... of K (together they read whole runs of B's rows), sends
-// every other CTA the rows of its sum that are that one's to finish (stores into its shared memory, then an arrival on
-// its mbarrier), and finishes its own share, adding the parts in rank order: no atomics, the same sum in every run.
+// every CTA the rows of its sum that are that one's to finish (a bulk copy into its shared memory), and finishes its own
+// share, adding the parts in rank order: no atomics, the same sum in every run.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
 #include <algorithm>
 #include <atomic>
@@ -83,37 +83,51 @@ __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t parts,
 #pragma unroll
             for (int x = 0; x < S; ++x)
                 part[i][x] = shared_load(parts + (uint32_t)((x * per + min(r0 + i, per - 1)) * kTileN + 4 * lane) * 4u);
+        float v[R][4];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            float v[4] = {part[i][0].x, part[i][0].y, part[i][0].z, part[i][0].w};
+            v[i][0] = part[i][0].x; v[i][1] = part[i][0].y; v[i][2] = part[i][0].z; v[i][3] = part[i][0].w;
 #pragma unroll
             for (int x = 1; x < S; ++x) {
-                v[0] += part[i][x].x; v[1] += part[i][x].y; v[2] += part[i][x].z; v[3] += part[i][x].w;
+                v[i][0] += part[i][x].x; v[i][1] += part[i][x].y; v[i][2] += part[i][x].z; v[i][3] += part[i][x].w;
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += bias[j];
-            if (p.act == SVDCACHE_ACT_GELU) {
-                pair_to(gelu_tanh(pair_of(v[0], v[1])), v[0], v[1]);
-                pair_to(gelu_tanh(pair_of(v[2], v[3])), v[2], v[3]);
+            for (int j = 0; j < 4; ++j) v[i][j] += bias[j];
+        }
+        if (p.act == SVDCACHE_ACT_GELU) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                pair_to(gelu_tanh(pair_of(v[i][0], v[i][1])), v[i][0], v[i][1]);
+                pair_to(gelu_tanh(pair_of(v[i][2], v[i][3])), v[i][2], v[i][3]);
             }
-            const int64_t m = m_first + r0 + i;
-            const bool live = r0 + i < rows;
-            if (p.out != SVDCACHE_FP8) {
-                if (live) store_plain(p, m, n, v);
-                continue;
-            }
-            float top = 0.0f;
+        }
+        if (p.out != SVDCACHE_FP8) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (r0 + i < rows) store_plain(p, m_first + r0 + i, n, v[i]);
+            continue;
+        }
+        float top[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            top[i] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = n + j < p.N ? fp8_nan_if_not_finite(v[j]) : 0.0f;
-                top = fmaxf(top, fabsf(v[j]));
+                v[i][j] = n + j < p.N ? fp8_nan_if_not_finite(v[i][j]) : 0.0f;
+                top[i] = fmaxf(top[i], fabsf(v[i][j]));
             }
+        }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const uint32_t byte = fp8_scale_byte(top);
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < R; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], o));
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const uint32_t byte = fp8_scale_byte(top[i]);
             const float inv = fp8_inverse_scale(byte);
-            const uint32_t w = fp8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-            if (!live) continue;
+            const uint32_t w = fp8_pack4(v[i][0] * inv, v[i][1] * inv, v[i][2] * inv, v[i][3] * inv);
+            if (r0 + i >= rows) break;
+            const int64_t m = m_first + r0 + i;
             uint8_t *o = reinterpret_cast<uint8_t *>(p.C) + m * p.ldc + n;
             if (n + 4 <= p.N) *reinterpret_cast<uint32_t *>(o) = w;
             else
@@ -155,15 +169,17 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const int n_tile = tile % p.n_tiles;
     const int64_t m0 = (int64_t)(tile / p.n_tiles) * p.tile_m;
     const int count = (p.groups - rank + S - 1) / S;                    // groups rank, rank + S, ... of K: at least one
-    // the sums to finish: where the ring was (one CTA per tile: all of its loads have been consumed), or behind it
-    const uint32_t parts = S == 1 ? base : base + (uint32_t)p.stages * p.stage_bytes;
+    // the CTA's own sum goes where the ring was (all loads have been consumed by then); the parts that others send, behind
+    // both
+    const uint32_t parts = S == 1 ? base : base + max((uint32_t)p.stages * p.stage_bytes, (uint32_t)p.tile_m * kTileN * 4u);
 
     if (warp == 0 && elect_one()) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done_bar, 1);
-        mbar_init(parts_bar, 4 * S);                                    // four warps of every CTA
+        mbar_init(parts_bar, 1);
         abort_mem = 0;
         fence_barrier_init();
+        if (S > 1) mbar_arrive_expect_tx(parts_bar, (uint32_t)p.tile_m * kTileN * 4u);   // this CTA's rows from all S of them
         prefetch_tensormap(&tm_a);
         prefetch_tensormap(&tm_b);
     }
@@ -237,7 +253,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     // every wait below is passed by all CTAs of the cluster in the same order, also after a time-out in one of them
     if (S > 1) cluster_wait();                                          // the other CTAs' barriers exist
     if (warp >= 2) {
-        const int q = warp & 3, shift = 31 - __clz(p.tile_m / S);        // runs of a power of two of rows
+        const int q = warp & 3;
         const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(done_bar, 0u, abort_flag, 3));
         tc_fence_after();
         for (int c = 0; ok && c < p.tile_m; c += 32) {
@@ -245,17 +261,19 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             tmem_ld_32x32(tmem + ((uint32_t)(q * 32) << 16) + c, acc);
             tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                if (c + i >= p.tile_m) continue;
-                const int owner = (c + i) >> shift, row = (rank << shift) + (c + i) - (owner << shift);
-                const uint32_t at = parts + (uint32_t)(row * kTileN + q * 32 + lane) * 4u;
-                cluster_store(S > 1 ? cluster_addr(at, (uint32_t)owner) : at, __uint_as_float(acc[i]));
-            }
+            for (int i = 0; i < 32; ++i)
+                if (c + i < p.tile_m) shared_store1(base + (uint32_t)((c + i) * kTileN + q * 32 + lane) * 4u, acc[i]);
         }
         tc_fence_before();
         if (S > 1) {
-            __syncwarp();
-            if (lane < S) mbar_arrive_cluster(cluster_addr(parts_bar, (uint32_t)lane));
+            fence_proxy_async();
+            named_barrier(1, 128);
+            if (warp == 2 && lane < S) {        // to CTA `lane`: its rows of this CTA's sum
+                const uint32_t run = (uint32_t)(p.tile_m / S * kTileN) * 4u;
+                bulk_send(cluster_addr(parts + (uint32_t)rank * run, (uint32_t)lane), base + (uint32_t)lane * run, run,
+                          cluster_addr(parts_bar, (uint32_t)lane));
+                tma_store_commit();
+            }
         }
     }
     __syncthreads();
@@ -279,6 +297,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         case 4: finish_rows<4, 2>(p, parts, rank, m0, n_tile, bias); break;
         default: finish_rows<8, 1>(p, parts, rank, m0, n_tile, bias); break;
     }
+    if (S > 1 && warp == 2) tma_store_wait_read<0>();                   // what this CTA sent has left its shared memory
 }
 
 // ---------------------------------------------------------------------- pairs of CTAs ---
@@ -796,7 +815,7 @@ int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + 1024u;
     p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
-    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // one CTA per tile: they pass through the ring
+    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // pass through the ring, and with several CTAs per tile arrive behind it
     const size_t room = t.shared_sm ? kSmemLimit / 2 : kSmemLimit;
     static_assert((kSmemLimit / 2 - 1024 - 64 * kTileN * 4) / (kBBytes + 64 * kStageK + 1024) >= 2 &&
                   (kSmemLimit - 1024 - 128 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
@@ -805,7 +824,7 @@ int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     const int longest = (p.groups + p.splits - 1) / p.splits;
     if (p.stages > longest) p.stages = longest;
     size_t smem = (size_t)p.stages * p.stage_bytes;
-    smem = 1024 + (p.splits > 1 ? smem + sums : smem > sums ? smem : sums);
+    smem = 1024 + std::max(smem, sums) + (p.splits > 1 ? sums : 0);
 
     CUtensorMap tm_a, tm_b;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);

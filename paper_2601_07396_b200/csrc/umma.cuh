@@ -182,20 +182,23 @@ __device__ __forceinline__ float4 shared_load(uint32_t addr) {
 __device__ __forceinline__ void shared_store(uint32_t addr, const uint32_t (&w)[4]) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
-__device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+// copy from this CTA's shared memory to another's of the cluster, counted in bytes on an mbarrier there (both addresses
+// from cluster_addr); a bulk async group reads the source
+__device__ __forceinline__ void bulk_send(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "r"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
-// arrival on an mbarrier of another CTA of the cluster (an address from cluster_addr), after this thread's memory
-// operations
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// The same where there is no memory to publish, only tensor memory that has been read (tcgen05.wait::ld and
-// tc_fence_before() come before it): without the release, which waits 2000-3500 cycles for the stores under way.
+__device__ __forceinline__ void shared_store1(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+// barrier of `threads` threads of the CTA (whole warps), by number
+__device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// arrival on an mbarrier of another CTA of the cluster (an address from cluster_addr) where there is no memory to
+// publish, only tensor memory that has been read (tcgen05.wait::ld and tc_fence_before() come before it).  The release of
+// the plain form waits 2000-3500 cycles for the stores under way.
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// Bounded wait for arrivals from the whole cluster and the shared-memory stores before them.  It does not give up when
+// Bounded wait for what other CTAs of the cluster send to this one's shared memory.  It does not give up when
 // another thread has: whoever else holds this CTA's addresses must be done with them before the CTA leaves.
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
