@@ -118,9 +118,7 @@ __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t parts,
             }
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < R; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], o));
+        for (int i = 0; i < R; ++i) top[i] = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top[i])));   // none is negative
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const uint32_t byte = fp8_scale_byte(top[i]);
@@ -713,7 +711,9 @@ EncodeTiledFn encode_fn() {
 }
 
 // bytes [rows x cols], rows `ld` bytes apart, boxes of 128 bytes x box_rows with the 128-byte swizzle; bytes
-// beyond the matrix read as zero, which is e4m3's zero
+// beyond the matrix read as zero, which is e4m3's zero.  Where rows begin at multiples of 256 bytes, L2 fetches so many
+// at a time, two groups of K that are read one after the other (1 x 18432 x 9216 31.7 -> 29.5 us); elsewhere half of such
+// a fetch may belong to another row (256 x 6912 x 9000 27.1 -> 29.3 us, 40 x 18432 x 400 4.8 -> 5.2).
 int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t ld, int box_rows) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return SVDCACHE_ERR_CUDA;
@@ -722,7 +722,8 @@ int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t l
     const cuuint32_t box[2] = {(cuuint32_t)kStageK, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          ld % 256 == 0 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
@@ -892,15 +893,17 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
                         tm_sb, tm_c, p);
 }
 
-// Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4096,
-// N from 128 to 18432, K from 100 to 12288; the choice is within 7 % of the better one but for a few shapes):
+// Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4000,
+// N from 128 to 18432, K from 100 to 9216; over 428 shapes the choice takes 0.4 % more than the best one on average, 15 % at
+// most):
 //   pairs       3.1 us from launch to end, and per round of the clusters 0.4 and for a group of K 0.20 us at BN = 128, 0.23
 //               at 192, 0.35 at 256, two fifths more where rows do not begin at multiples of 128 bytes (a box's row then
 //               lies in two lines); or 4 us and B's bytes at 4 TB/s, where that is more: a pair's ring holds little of B
-//   small tiles 3.8 us up to 16 rows, else 5.7 (0.6 more for 8-bit C), and per group of a CTA's share of K 0.36 us, 0.55 at
-//               128 rows, 0.6 where two CTAs share an SM; or 4.5 us and B's bytes at 6 TB/s
-// K = 100, N = 512, M = 64: 3.9 us by pairs, 6.2 by small tiles.  K = 9000, N = 512, M = 1 / 64 / 512: 15.9 / 19.1 / 23.7
-// and 7.5 / 9.5 / 12.7.  K = 3072, N = 18432, M = 1 / 64 / 256: 24.7 / 16.2 / 18.1 and 14.0 / 15.6 / 35.0.
+//   small tiles 1.8 us up to 16 rows, 3.1 up to 64, 4.2 at 128; 1 more where CTAs exchange sums; 0.7 more for 8-bit C, 1.2
+//               where one CTA finishes a tile of more than 16 rows; and per group of a CTA's share of K 0.35 us, 0.45
+//               at 128 rows; or 3.5 us and B's bytes at 6 TB/s
+// N = 500, K = 100, M = 40: 3.7 us by pairs, 3.4 by small tiles (into 8 bits 4.5 and 4.4).  N = 500, K = 9000, M = 1 / 40 / 512:
+// 16.0 / 17.7 / 24.2 and 6.6 / 7.8 / 11.1.  N = 18432, K = 3072, M = 1 / 40 / 256: 22.6 / 19.2 / 17.6 and 12.9 / 13.6 / 25.0.
 struct PairPlan {
     int bn;
     int64_t time;
@@ -922,9 +925,10 @@ int64_t tile_time(const GemmFp8Args &a, const TilePlan &t, const Device &d) {
     int log = 0;
     while (1 << log < t.splits) ++log;
     const int64_t fit = d.clusters[t.tile_m <= 64][log], rounds = (t.tiles + fit - 1) / fit;
-    const int64_t base = (t.tile_m == 16 ? 380 : 570) + (a.out == SVDCACHE_FP8 ? 60 : 0), each = (t.groups + t.splits - 1) / t.splits;
-    const int64_t group = t.tile_m == 128 ? 55 : t.tiles * t.splits <= d.sms ? 36 : 60;
-    return std::max(base + rounds * each * group, 450 + (int64_t)a.N * a.K / 60000);
+    const int64_t base = t.tile_m == 16 ? 180 : t.tile_m <= 64 ? 310 : 420, exchange = t.splits > 1 ? 100 : 0;
+    const int64_t bytes = a.out != SVDCACHE_FP8 ? 0 : t.splits == 1 && t.tile_m > 16 ? 120 : 70;
+    const int64_t each = (t.groups + t.splits - 1) / t.splits, group = t.tile_m == 128 ? 45 : 35;
+    return std::max(base + exchange + bytes + rounds * each * group, 350 + (int64_t)a.N * a.K / 60000);
 }
 
 }  // namespace
