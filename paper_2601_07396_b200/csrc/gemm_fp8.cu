@@ -422,15 +422,29 @@ __device__ __forceinline__ void send_box(const CUtensorMap *tm_c, const PairPara
                 const int left = p.N - n - c * kPiece;       // columns from this piece on
                 if (left <= 0) break;
                 const float4 f = shared_load(box + (uint32_t)lane * 128u + (uint32_t)(c ^ (lane & 7)) * 16u);
-                T v[kPiece];
-                memcpy(v, &f, 16);
+                T *o = out + c * kPiece;
                 if (left >= kPiece) {
-                    *reinterpret_cast<float4 *>(out + c * kPiece) = f;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kPiece; ++i)
-                        if (i < left) out[c * kPiece + i] = v[i];
+                    *reinterpret_cast<float4 *>(o) = f;
+                    continue;
                 }
+                // the first left * sizeof(T) bytes: 8, 4, 2 and 1 of them, as that number's bits say
+                uint32_t w[4];
+                memcpy(w, &f, 16);
+                const int bytes = left * (int)sizeof(T);
+                uint8_t *b = reinterpret_cast<uint8_t *>(o);
+                if (bytes & 8) {
+                    *reinterpret_cast<uint2 *>(b) = make_uint2(w[0], w[1]);
+                    w[0] = w[2]; w[1] = w[3]; b += 8;
+                }
+                if (bytes & 4) {
+                    *reinterpret_cast<uint32_t *>(b) = w[0];
+                    w[0] = w[1]; b += 4;
+                }
+                if (bytes & 2) {
+                    *reinterpret_cast<uint16_t *>(b) = (uint16_t)w[0];
+                    w[0] >>= 16; b += 2;
+                }
+                if (bytes & 1) *b = (uint8_t)w[0];
             }
         }
         __syncwarp();
@@ -602,8 +616,12 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 for (int j = 0; j < 4; ++j) add_bias_and_act<32>(v + 32 * j, bias + 32 * j, p.act);
                 if (col0 + 128 > p.N) {
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (col0 + i >= p.N) v[i] = 0.0f;
+                    for (int j = 0; j < 128; j += 32) {
+                        if (col0 + j + 32 <= p.N) continue;
+#pragma unroll
+                        for (int i = j; i < j + 32; ++i)
+                            if (col0 + i >= p.N) v[i] = 0.0f;
+                    }
                 }
                 float top = largest_of(v);
                 if (__float_as_uint(top) == 0x7F800000u) {
