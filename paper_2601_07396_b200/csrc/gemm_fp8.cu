@@ -67,14 +67,15 @@ __device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int 
     }
 }
 
-// The rows of a tile are dealt to its cluster's S CTAs in runs of tile_m / S, and within a CTA to the warps, R at a
-// time, four columns per lane.  `parts`: S blocks [tile_m / S][128] of sums, one from every CTA.
+// The rows of a tile are dealt to its cluster's S CTAs in runs of ceil(tile_m / S), and within a CTA to the warps, R at a
+// time, four columns per lane.  `parts`: S blocks [run][128] of sums, one from every CTA.
 template <int S, int R>
 __device__ __forceinline__ void finish_rows(const TileParams &p, uint32_t parts, int rank, int64_t m0, int n_tile, const float (&bias)[4]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int per = p.tile_m / S;
+    const int per = (p.tile_m + S - 1) / S;
     const int64_t m_first = m0 + rank * per;
-    const int rows = (int)(p.M - m_first < per ? p.M - m_first : per);
+    const int own = min(per, p.tile_m - rank * per);
+    const int rows = (int)(p.M - m_first < own ? p.M - m_first : own);
     const int n = n_tile * kTileN + 4 * lane;
     for (int r0 = warp * R; r0 < rows; r0 += kTileThreads / 32 * R) {
         float4 part[R][S];
@@ -167,6 +168,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const int n_tile = tile % p.n_tiles;
     const int64_t m0 = (int64_t)(tile / p.n_tiles) * p.tile_m;
     const int count = (p.groups - rank + S - 1) / S;                    // groups rank, rank + S, ... of K: at least one
+    const int per = (p.tile_m + S - 1) / S, own = min(per, p.tile_m - rank * per);   // rows that a CTA finishes
     // the CTA's own sum goes where the ring was (all loads have been consumed by then); the parts that others send, behind
     // both
     const uint32_t parts = S == 1 ? base : base + max((uint32_t)p.stages * p.stage_bytes, (uint32_t)p.tile_m * kTileN * 4u);
@@ -177,7 +179,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         mbar_init(parts_bar, 1);
         abort_mem = 0;
         fence_barrier_init();
-        if (S > 1) mbar_arrive_expect_tx(parts_bar, (uint32_t)p.tile_m * kTileN * 4u);   // this CTA's rows from all S of them
+        if (S > 1) mbar_arrive_expect_tx(parts_bar, (uint32_t)(S * own) * kTileN * 4u);   // this CTA's rows from all S of them
         prefetch_tensormap(&tm_a);
         prefetch_tensormap(&tm_b);
     }
@@ -271,8 +273,8 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             fence_proxy_async();
             named_barrier(1, 128);
             if (warp == 2 && lane < S) {        // to CTA `lane`: its rows of this CTA's sum
-                const uint32_t run = (uint32_t)(p.tile_m / S * kTileN) * 4u;
-                bulk_send(cluster_addr(parts + (uint32_t)rank * run, (uint32_t)lane), base + (uint32_t)lane * run, run,
+                const uint32_t run = (uint32_t)(per * kTileN) * 4u, last = (uint32_t)((p.tile_m - lane * per) * kTileN) * 4u;
+                bulk_send(cluster_addr(parts + (uint32_t)rank * run, (uint32_t)lane), base + (uint32_t)lane * run, min(run, last),
                           cluster_addr(parts_bar, (uint32_t)lane));
                 tma_store_commit();
             }
@@ -296,7 +298,9 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     switch (S) {
         case 1: finish_rows<1, 4>(p, parts, rank, m0, n_tile, bias); break;
         case 2: finish_rows<2, 4>(p, parts, rank, m0, n_tile, bias); break;
+        case 3: finish_rows<3, 2>(p, parts, rank, m0, n_tile, bias); break;
         case 4: finish_rows<4, 2>(p, parts, rank, m0, n_tile, bias); break;
+        case 6: finish_rows<6, 1>(p, parts, rank, m0, n_tile, bias); break;
         default: finish_rows<8, 1>(p, parts, rank, m0, n_tile, bias); break;
     }
     if (S > 1 && warp == 2) tma_store_wait_read<0>();                   // what this CTA sent has left its shared memory
@@ -753,10 +757,13 @@ int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t l
     return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
 }
 
-// What the launches ask of a device, once: its SMs, how many clusters of 1, 2, 4, 8 CTAs of tile_kernel it runs at the
-// same time with all or half of an SM's shared memory per CTA, and leave to use that much.
+// CTAs per tile of tile_kernel.  (3 and 6 for numbers of tiles that leave SMs to 2 and 4: 256 x 1152 x 9000 16.6 -> 13.2 us.)
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8}, kSplitKinds = 6;
+
+// What the launches ask of a device, once: its SMs, how many clusters of so many CTAs of tile_kernel it runs at the same
+// time, and leave to use an SM's shared memory.
 struct Device {
-    int sms, clusters[2][4];
+    int sms, clusters[kSplitKinds];
 };
 constexpr int kMaxDevices = 64;
 
@@ -768,20 +775,19 @@ int ask_device(Device *d) {
                           (const void *)pair_kernel<SVDCACHE_BF16, 128>, (const void *)pair_kernel<SVDCACHE_BF16, 192>,
                           (const void *)pair_kernel<SVDCACHE_FP8, 128>, (const void *)pair_kernel<SVDCACHE_FP8, 256>})
         if (!rc) rc = record_cuda(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-    for (int half = 0; half < 2; ++half)
-        for (int i = 0; i < 4 && !rc; ++i) {
-            cudaLaunchConfig_t cfg{};
-            cudaLaunchAttribute attr[1];
-            cfg.gridDim = dim3(8 * (unsigned)d->sms);
-            cfg.blockDim = dim3(kTileThreads);
-            cfg.dynamicSmemBytes = kSmemLimit >> half;
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = 1u << i;
-            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = 1;
-            rc = record_cuda(cudaOccupancyMaxActiveClusters(&d->clusters[half][i], tile_kernel, &cfg));
-        }
+    for (int i = 0; i < kSplitKinds && !rc; ++i) {
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute attr[1];
+        cfg.gridDim = dim3(24 * (unsigned)d->sms);
+        cfg.blockDim = dim3(kTileThreads);
+        cfg.dynamicSmemBytes = kSmemLimit;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)kSplits[i];
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        rc = record_cuda(cudaOccupancyMaxActiveClusters(&d->clusters[i], tile_kernel, &cfg));
+    }
     return rc;
 }
 
@@ -807,28 +813,8 @@ int device(Device *d) {
 // How tile_kernel would take a product.
 struct TilePlan {
     int tile_m, splits, n_tiles, groups;
-    int64_t tiles;
-    bool shared_sm;          // more CTAs than SMs: half of the shared memory each
+    int64_t tiles, time;
 };
-
-TilePlan plan_tile(const GemmFp8Args &a, const Device &d) {
-    TilePlan t{};
-    t.groups = (int)fp8_groups(a.K);
-    t.n_tiles = (a.N + kTileN - 1) / kTileN;
-    // Rows per tile: what M needs, up to 128, or 64 where that still leaves SMs idle.  (Fewer only where M has no more:
-    // an MMA's scale words begin at an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
-    t.tile_m = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-    if (t.tile_m == 128 && (a.M + 127) / 128 * t.n_tiles * 2 <= d.sms) t.tile_m = 64;
-    t.tiles = (a.M + t.tile_m - 1) / t.tile_m * t.n_tiles;
-    // CTAs per tile: as many as keep two groups of K each, while all clusters still run at the same time: with one CTA
-    // an SM, or two where a tile has at most 64 rows, for which half of the shared memory still makes a ring.
-    const bool halves = t.tile_m <= 64;
-    int log = 0;
-    while (log < 3 && t.tiles <= d.clusters[halves][log + 1] && t.groups >= 4 << log) ++log;
-    t.splits = 1 << log;
-    t.shared_sm = halves && t.tiles > d.clusters[0][log];
-    return t;
-}
 
 int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     TileParams p{};
@@ -841,16 +827,15 @@ int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + 1024u;
     p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
-    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // pass through the ring, and with several CTAs per tile arrive behind it
-    const size_t room = t.shared_sm ? kSmemLimit / 2 : kSmemLimit;
-    static_assert((kSmemLimit / 2 - 1024 - 64 * kTileN * 4) / (kBBytes + 64 * kStageK + 1024) >= 2 &&
-                  (kSmemLimit - 1024 - 128 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
-    p.stages = (int)((room - 1024 - (p.splits > 1 ? sums : 0)) / p.stage_bytes);
+    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // pass through the ring,
+    const size_t parts = p.splits == 1 ? 0 : (size_t)((p.tile_m + p.splits - 1) / p.splits * p.splits) * kTileN * 4;   // others' arrive behind it
+    static_assert((kSmemLimit - 1024 - 132 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
+    p.stages = (int)((kSmemLimit - 1024 - parts) / p.stage_bytes);
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     const int longest = (p.groups + p.splits - 1) / p.splits;
     if (p.stages > longest) p.stages = longest;
     size_t smem = (size_t)p.stages * p.stage_bytes;
-    smem = 1024 + std::max(smem, sums) + (p.splits > 1 ? sums : 0);
+    smem = 1024 + std::max(smem, sums) + parts;
 
     CUtensorMap tm_a, tm_b;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
@@ -919,16 +904,16 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
 }
 
 // Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4000,
-// N from 128 to 18432, K from 100 to 9216; over 428 shapes the choice takes 0.4 % more than the best one on average, 15 % at
-// most):
+// N from 128 to 18432, K from 100 to 9216; over 698 shapes the choice takes 1-2 % more than the best of all on average and
+// up to a fifth at a few):
 //   pairs       3.1 us from launch to end, and per round of the clusters 0.4 and for a group of K 0.20 us at BN = 128, 0.23
 //               at 192, 0.35 at 256, two fifths more where rows do not begin at multiples of 128 bytes (a box's row then
 //               lies in two lines); or 4 us and B's bytes at 4 TB/s, where that is more: a pair's ring holds little of B
-//   small tiles 1.8 us up to 16 rows, 3.1 up to 64, 4.2 at 128; 1 more where CTAs exchange sums; 0.7 more for 8-bit C, 1.2
-//               where one CTA finishes a tile of more than 16 rows; and per group of a CTA's share of K 0.35 us, 0.45
-//               at 128 rows; or 3.5 us and B's bytes at 6 TB/s
-// N = 500, K = 100, M = 40: 3.7 us by pairs, 3.4 by small tiles (into 8 bits 4.5 and 4.4).  N = 500, K = 9000, M = 1 / 40 / 512:
-// 16.0 / 17.7 / 24.2 and 6.6 / 7.8 / 11.1.  N = 18432, K = 3072, M = 1 / 40 / 256: 22.6 / 19.2 / 17.6 and 12.9 / 13.6 / 25.0.
+//   small tiles 2.1 us, 1.5 us per 100 rows of a tile and 0.4 (8-bit C: 1.5) per 100 rows that a CTA finishes, 1.2 more where
+//               CTAs exchange sums; and per group of a CTA's share of K 0.20 us at 16 rows, 0.32 at 64, 0.48 at 128, or
+//               B's bytes at 5.6 TB/s, where that is more
+// N = 500, K = 100, M = 40: 3.9 us by pairs, 3.8 by small tiles.  N = 500, K = 9000, M = 1 / 40 / 512: 15.0 / 17.7 / 24.3 and
+// 6.2 / 7.4 / 11.2.  N = 18432, K = 3072, M = 1 / 40 / 256: 27.0 / 21.7 / 16.8 and 12.0 / 12.8 / 24.4.
 struct PairPlan {
     int bn;
     int64_t time;
@@ -946,14 +931,25 @@ PairPlan plan_pair(const GemmFp8Args &a, const Device &d) {
     return t_wide < t_128 ? PairPlan{wide, t_wide} : PairPlan{128, t_128};
 }
 
-int64_t tile_time(const GemmFp8Args &a, const TilePlan &t, const Device &d) {
-    int log = 0;
-    while (1 << log < t.splits) ++log;
-    const int64_t fit = d.clusters[t.tile_m <= 64][log], rounds = (t.tiles + fit - 1) / fit;
-    const int64_t base = t.tile_m == 16 ? 180 : t.tile_m <= 64 ? 310 : 420, exchange = t.splits > 1 ? 100 : 0;
-    const int64_t bytes = a.out != SVDCACHE_FP8 ? 0 : t.splits == 1 && t.tile_m > 16 ? 120 : 70;
-    const int64_t each = (t.groups + t.splits - 1) / t.splits, group = t.tile_m == 128 ? 45 : 35;
-    return std::max(base + exchange + bytes + rounds * each * group, 350 + (int64_t)a.N * a.K / 60000);
+TilePlan plan_tile(const GemmFp8Args &a, const Device &d) {
+    TilePlan best{};
+    const int groups = (int)fp8_groups(a.K), n_tiles = (a.N + kTileN - 1) / kTileN;
+    // Rows per tile: what M needs, up to 64 or 128.  (Fewer only where M has no more: an MMA's scale words begin at an even
+    // column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
+    const int least = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64, most = a.M <= 64 ? least : 128;
+    for (int tile_m = least; tile_m <= most; tile_m *= 2) {
+        const int64_t tiles = (a.M + tile_m - 1) / tile_m * n_tiles;
+        // CTAs per tile: such that all clusters run at the same time and each CTA has two groups of K
+        for (int i = 0; i < kSplitKinds; ++i) {
+            const int splits = kSplits[i], fit = d.clusters[i];
+            if (i > 0 && (tiles > fit || groups < 2 * splits)) break;
+            const int own = (tile_m + splits - 1) / splits, each = (groups + splits - 1) / splits;
+            const int64_t ends = 210 + (splits > 1 ? 120 : 0) + tile_m * 3 / 2 + (a.out == SVDCACHE_FP8 ? own * 3 / 2 : own * 2 / 5);
+            const int64_t time = ends + std::max((tiles + fit - 1) / fit * each * (16 + tile_m / 4), (int64_t)a.N * a.K / 56000);
+            if (!best.splits || time < best.time) best = {tile_m, splits, n_tiles, groups, tiles, time};
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -964,7 +960,7 @@ int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
     if (rc) return rc;
     const TilePlan t = plan_tile(a, d);
     const PairPlan p = plan_pair(a, d);
-    if (tile_time(a, t, d) < p.time) return tile_launch(a, t, s);
+    if (t.time < p.time) return tile_launch(a, t, s);
     const int clusters = d.sms / 2;
     if (a.out == SVDCACHE_FP8) return p.bn == 256 ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
     if (a.out == SVDCACHE_BF16) return p.bn == 192 ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);

@@ -220,6 +220,15 @@ def test_product_with_every_epilogue(M, N, K, out, act, has_bias):
     run_product(M, N, K, out, act, has_bias, seed=K, tile_rows=1)
 
 
+# few tiles and a long sum, so that 3, 4, 6 or 8 CTAs share a tile of 16, 32, 64 or 128 rows, evenly or not
+@gpu
+@pytest.mark.parametrize("M,N,K", [(3, 130, 1100), (11, 130, 1540), (16, 260, 2000), (20, 130, 800), (31, 130, 1540), (32, 400, 2100), (50, 130, 800),
+                                   (64, 130, 1540), (100, 2100, 1100), (100, 2100, 6000), (200, 1500, 4100), (193, 2500, 2600), (260, 130, 2000)])
+def test_product_of_tiles_that_ctas_share(M, N, K):
+    run_product(M, N, K, "f32", seed=N + K)
+    run_product(M, N, K, "fp8", sc.ACT_GELU, True, seed=N)
+
+
 @gpu
 @pytest.mark.parametrize("out", ["bf16", "fp8"])
 def test_product_at_the_widths_of_the_streams(out):
