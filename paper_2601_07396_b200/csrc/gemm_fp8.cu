@@ -10,7 +10,7 @@
 // C, so that few rows of C waste no tensor work.  One CTA per tile; where that leaves SMs idle, the S CTAs of a
 // cluster share a tile: CTA r takes the groups r, r + S, ... of K (together they read whole runs of B's rows), sends
 // every CTA the rows of its sum that are that one's to finish (a bulk copy into its shared memory), and finishes its own
-// share, adding the parts in rank order: no atomics, the same sum in every run.
+// share, adding the parts in rank order: no atomics, the same sum in every run.  No CTA leaves before all have their parts.
 // Warps: 0 TMA producer, 1 MMA issuer, 2-5 accumulator -> shared memory; then all of them write C.
 #include <algorithm>
 #include <atomic>
@@ -276,7 +276,6 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 const uint32_t run = (uint32_t)(per * kTileN) * 4u, last = (uint32_t)((p.tile_m - lane * per) * kTileN) * 4u;
                 bulk_send(cluster_addr(parts + (uint32_t)rank * run, (uint32_t)lane), base + (uint32_t)lane * run, min(run, last),
                           cluster_addr(parts_bar, (uint32_t)lane));
-                tma_store_commit();
             }
         }
     }
@@ -295,6 +294,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         }
     }
     __syncwarp();
+    if (S > 1) cluster_arrive();                                        // this CTA has all its parts (or has waited long enough)
     switch (S) {
         case 1: finish_rows<1, 4>(p, parts, rank, m0, n_tile, bias); break;
         case 2: finish_rows<2, 4>(p, parts, rank, m0, n_tile, bias); break;
@@ -303,7 +303,10 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         case 6: finish_rows<6, 1>(p, parts, rank, m0, n_tile, bias); break;
         default: finish_rows<8, 1>(p, parts, rank, m0, n_tile, bias); break;
     }
-    if (S > 1 && warp == 2) tma_store_wait_read<0>();                   // what this CTA sent has left its shared memory
+    // What a CTA sent is reported to the receiver alone: only when every CTA has its parts has this one's shared memory been
+    // read to the end, and may go to another CTA.
+    __syncwarp();
+    if (S > 1) cluster_wait();
 }
 
 // ---------------------------------------------------------------------- pairs of CTAs ---

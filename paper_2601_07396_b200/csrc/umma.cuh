@@ -182,8 +182,9 @@ __device__ __forceinline__ float4 shared_load(uint32_t addr) {
 __device__ __forceinline__ void shared_store(uint32_t addr, const uint32_t (&w)[4]) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
-// copy from this CTA's shared memory to another's of the cluster, counted in bytes on an mbarrier there (both addresses
-// from cluster_addr); a bulk async group reads the source
+// Copy from this CTA's shared memory to another's of the cluster, counted in bytes on an mbarrier there (both addresses
+// from cluster_addr).  That count is the only sign of its completion: it belongs to no bulk async group, so the sender
+// learns that its memory has been read from the receiver, and may not leave before.
 __device__ __forceinline__ void bulk_send(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "r"(src), "r"(bytes), "r"(bar)
