@@ -438,7 +438,8 @@ def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
 
 # The calls below can be shorter on the GPU than a binding in Python is on the host, so their arguments are read and
 # checked by a small extension (csrc/calls.cpp), which calls the same C entry points.  It raises ValueError for
-# arguments that the C ABI cannot see to be wrong (shapes against one another, device, contiguity).
+# arguments that the C ABI cannot see to be wrong (types, shapes against one another, device, contiguity).  The values of an
+# 8-bit matrix are uint8 or float8_e4m3fn tensors, its scales uint8 or float8_e8m0fnu.
 CALLS_PATH = os.path.join(_HERE, "_calls.so")
 _calls = None
 

@@ -53,14 +53,19 @@ struct Fp8 {
     int64_t ld;
 };
 
-// bytes of at least `cols` columns, and their scale buffer
+// Values as e4m3 or plain bytes, scales as E8M0 or plain bytes: other types of one byte (e5m2, int8, bool) would be read as
+// what they are not.
+bool holds_values(const at::Tensor &t) { return t.scalar_type() == at::kByte || t.scalar_type() == at::kFloat8_e4m3fn; }
+bool holds_scales(const at::Tensor &t) { return t.scalar_type() == at::kByte || t.scalar_type() == at::kFloat8_e8m0fnu; }
+
+// a matrix of at least `cols` columns, and its scale buffer
 Fp8 fp8(PyObject *qo, PyObject *so, int64_t rows, int64_t cols, int device, const char *what) {
     const at::Tensor &q = tensor(qo, what), &s = tensor(so, what);
     const Matrix m = matrix(q, device, what);
-    if (m.rows != rows || m.cols < cols || q.element_size() != 1) refuse(what, "a byte for each element is expected");
-    if (!s.is_cuda() || s.get_device() != device || s.element_size() != 1 || !s.is_contiguous() ||
+    if (m.rows != rows || m.cols < cols || !holds_values(q)) refuse(what, "a byte (uint8 or float8_e4m3fn) for each element is expected");
+    if (!s.is_cuda() || s.get_device() != device || !holds_scales(s) || !s.is_contiguous() ||
         s.numel() < (rows + 127) / 128 * ((cols + 511) / 512) * 512)
-        refuse(what, "a scale buffer of svdcache_fp8_scale_bytes(rows, cols) bytes is expected");
+        refuse(what, "a scale buffer of svdcache_fp8_scale_bytes(rows, cols) bytes (uint8 or float8_e8m0fnu) is expected");
     return {m.p, s.data_ptr(), m.ld};
 }
 
