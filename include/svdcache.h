@@ -356,7 +356,10 @@ SVDCACHE_API int svdcache_left_factors(const float *C, const double *sigma, int6
  *              sums fp32 in the tensor cores.  1 <= N, K <= 131072.
  *              status (device, one int32 that the caller sets to 0 once) receives
  *              SVDCACHE_ERR_TIMEOUT if a bounded in-kernel wait runs out; it is never cleared here.
- * All three only enqueue work on `stream`.  Results are bit-reproducible.
+ *   svdcache_gemm_fp8_status_word   the address of a status word that the library itself has on the
+ *              current device, zero when the library is loaded, for callers that keep none (the
+ *              Python binding's default); svdcache_gemm_fp8_status_query waits for the device and reads it.
+ * The three calls only enqueue work on `stream`, and any of them may be the first in a process to be captured.  Results are bit-reproducible.
  * ------------------------------------------------------------------------------- */
 #define SVDCACHE_ACT_NONE  0
 #define SVDCACHE_ACT_GELU  1   /* x / (1 + exp(-2u)), u = sqrt(2 / pi) (x + 0.044715 x^3) */
@@ -369,6 +372,8 @@ SVDCACHE_API int svdcache_residual_rmsnorm_fp8(const void *H, int64_t ldh, const
 SVDCACHE_API int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb,
                       const void *SB, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
                       void *SC, int64_t M, int N, int K, int32_t *status, void *stream);
+SVDCACHE_API int svdcache_gemm_fp8_status_word(int32_t **word /* host, out: a device address */);
+SVDCACHE_API int svdcache_gemm_fp8_status_query(int32_t *status /* host, out */);
 
 /* ---------------------------------------------------------------------------------
  * Introspection for benchmarks and tests (host only).

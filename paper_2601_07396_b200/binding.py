@@ -72,6 +72,8 @@ SIGNATURES = {
     "svdcache_quantize_fp8": (_ci, [_vp, _i64, _ci, _i64, _ci, _ci, _vp, _i64, _vp, _vp]),
     "svdcache_residual_rmsnorm_fp8": (_ci, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, ctypes.c_float, _vp, _i64, _vp, _i64,
                                             _ci, _ci, _vp]),
+    "svdcache_gemm_fp8_status_word": (_ci, [ctypes.POINTER(_vp)]),
+    "svdcache_gemm_fp8_status_query": (_ci, [ctypes.POINTER(ctypes.c_int32)]),
     "svdcache_gemm_fp8": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp]),
 }
 
@@ -426,8 +428,6 @@ def svdcache_left_factors(C: torch.Tensor, sigma: torch.Tensor, stream=None) -> 
 # ------------------------------------------------------------- 8-bit linear path ---
 
 ACT_NONE, ACT_GELU = 0, 1
-_gemm_status = {}    # device index -> address of the device's status word
-_status_words = []
 
 
 def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
@@ -454,7 +454,8 @@ def calls():
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
         L = lib()
-        module.bind(*[ctypes.cast(f, _vp).value for f in (L.svdcache_quantize_fp8, L.svdcache_residual_rmsnorm_fp8, L.svdcache_gemm_fp8)])
+        module.bind(*[ctypes.cast(f, _vp).value for f in (L.svdcache_quantize_fp8, L.svdcache_residual_rmsnorm_fp8, L.svdcache_gemm_fp8,
+                                                            L.svdcache_gemm_fp8_status_word)])
         _calls = module
     return _calls
 
@@ -482,30 +483,32 @@ def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: to
                       status: Optional[torch.Tensor] = None, stream=None) -> None:
     """C [M, N] = act(A B^T + bias) of the 8-bit matrices A [M, >= K] and B [N, >= K].  C is fp32 or bf16, or bytes
     (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
-    one per device, which gemm_status() reads."""
-    word = status.data_ptr() if status is not None else _gemm_status.get(C.get_device()) or _new_status(C)
+    the library's own on that device, which gemm_status() reads."""
+    word = None if status is None else status.data_ptr()
     rc = (_calls or calls()).gemm(A, SA, B, SB, K, C, S_out, bias, act, word, None if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "gemm_fp8")
 
 
-def _new_status(C: torch.Tensor) -> int:
-    """A zeroed status word for C's device, kept until the process ends; its address."""
-    if not C.is_cuda:
-        raise ValueError("C: a device matrix is expected")
-    word = torch.zeros(1, dtype=torch.int32, device=C.device)
-    torch.cuda.synchronize(C.device)   # the zero is there whatever stream the product runs on
-    _status_words.append(word)
-    return _gemm_status.setdefault(C.get_device(), word.data_ptr())
+def svdcache_gemm_fp8_status_word() -> int:
+    """The address of the current device's default status word."""
+    out = _vp()
+    _check(lib().svdcache_gemm_fp8_status_word(ctypes.byref(out)), "gemm_fp8_status_word")
+    return out.value
+
+
+def svdcache_gemm_fp8_status_query() -> int:
+    """The current device's default status word, once all work of the device is done."""
+    out = ctypes.c_int32(0)
+    _check(lib().svdcache_gemm_fp8_status_query(ctypes.byref(out)), "gemm_fp8_status_query")
+    return out.value
 
 
 def gemm_status(device="cuda") -> int:
     """The sticky status of the products on `device` that were given no status word (synchronises): 0, or -6 if a
     bounded wait ran out in one of them."""
-    device = torch.device(device)
-    torch.cuda.synchronize(device)
-    address = _gemm_status.get(torch.cuda.current_device() if device.index is None else device.index)
-    return next((int(w.item()) for w in _status_words if w.data_ptr() == address), 0)
+    with torch.cuda.device(device):
+        return svdcache_gemm_fp8_status_query()
 
 
 def new_fp8(rows: int, cols: int, device="cuda"):

@@ -501,6 +501,20 @@ int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B,
     return gemm_fp8_launch(a, (cudaStream_t)stream);
 }
 
+int svdcache_gemm_fp8_status_word(int32_t **word) {
+    if (!word) return SVDCACHE_ERR_INVALID_ARG;
+    return gemm_fp8_status_word(word);
+}
+
+int svdcache_gemm_fp8_status_query(int32_t *status) {
+    if (!status) return SVDCACHE_ERR_INVALID_ARG;
+    int *word = nullptr;
+    int rc = gemm_fp8_status_word(&word);
+    if (!rc) rc = record_cuda(cudaDeviceSynchronize());
+    if (!rc) rc = record_cuda(cudaMemcpy(status, word, sizeof(*status), cudaMemcpyDeviceToHost));
+    return rc;
+}
+
 /* Blocks of different rank in one call: consecutive blocks of equal rank form one batched launch. */
 int svdcache_full_step_ranked_batched(int nblocks, const void *F, int64_t ld, size_t F_stride, const void *basis,
                                       size_t basis_stride, void *state, size_t state_stride, float *C_out,

@@ -16,9 +16,11 @@ namespace {
 using QuantizeFn = decltype(&svdcache_quantize_fp8);
 using NormFn = decltype(&svdcache_residual_rmsnorm_fp8);
 using GemmFn = decltype(&svdcache_gemm_fp8);
+using StatusWordFn = decltype(&svdcache_gemm_fp8_status_word);
 QuantizeFn g_quantize = nullptr;
 NormFn g_norm = nullptr;
 GemmFn g_gemm = nullptr;
+StatusWordFn g_status_word = nullptr;
 
 struct Refusal {};   // a Python error is set
 
@@ -129,12 +131,13 @@ template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f) {
     return nullptr;
 }
 
-// bind(quantize, norm, gemm): addresses of the library's functions
+// bind(quantize, norm, gemm, status_word): addresses of the library's functions
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 3, [&]() -> PyObject * {
+    return guarded(n, 4, [&]() -> PyObject * {
         g_quantize = reinterpret_cast<QuantizeFn>(static_cast<uintptr_t>(number(a[0])));
         g_norm = reinterpret_cast<NormFn>(static_cast<uintptr_t>(number(a[1])));
         g_gemm = reinterpret_cast<GemmFn>(static_cast<uintptr_t>(number(a[2])));
+        g_status_word = reinterpret_cast<StatusWordFn>(static_cast<uintptr_t>(number(a[3])));
         Py_RETURN_NONE;
     });
 }
@@ -176,7 +179,7 @@ PyObject *norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// gemm(A, SA, B, SB, K, C, S_out or None, bias or None, act, address of the status word, stream)
+// gemm(A, SA, B, SB, K, C, S_out or None, bias or None, act, address of the status word or None: the library's own, stream)
 PyObject *gemm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 11, [&] {
         const at::Tensor &c = tensor(a[5], "C");
@@ -194,9 +197,11 @@ PyObject *gemm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         } else {
             out = plain_type(c, "C");
         }
-        int32_t *status = reinterpret_cast<int32_t *>(static_cast<uintptr_t>(number(a[9])));
+        int32_t *status = a[9] == Py_None ? nullptr : reinterpret_cast<int32_t *>(static_cast<uintptr_t>(number(a[9])));
         void *stream = stream_of(a[10], dev);
         return call(dev, [&] {
+            const int rc = status ? SVDCACHE_OK : g_status_word(&status);
+            if (rc) return rc;
             return g_gemm(A.q, A.ld, A.s, B.q, B.ld, B.s, bias, act, m.p, m.ld, out, sc, m.rows, dim32(m.cols), dim32(K), status, stream);
         });
     });

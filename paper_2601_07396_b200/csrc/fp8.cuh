@@ -143,5 +143,6 @@ struct GemmFp8Args {
     int *status;            // device word that receives SVDCACHE_ERR_TIMEOUT if a bounded wait runs out
 };
 int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s);
+int gemm_fp8_status_word(int **word);   // the current device's default status word
 
 }  // namespace svdc

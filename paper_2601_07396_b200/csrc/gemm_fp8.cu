@@ -763,16 +763,22 @@ int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t l
 // CTAs per tile of tile_kernel.  (3 and 6 for numbers of tiles that leave SMs to 2 and 4: 256 x 1152 x 9000 16.6 -> 13.2 us.)
 constexpr int kSplits[] = {1, 2, 3, 4, 6, 8}, kSplitKinds = 6;
 
+// The status word of products that are given none: part of the library's image on each device, zero when that is loaded, so
+// that no first call has to allocate one or wait for its zero (which a stream capture forbids).
+__device__ int default_status;
+
 // What the launches ask of a device, once: its SMs, how many clusters of so many CTAs of tile_kernel it runs at the same
-// time, and leave to use an SM's shared memory.
+// time, where the default status word lies, and leave to use an SM's shared memory.
 struct Device {
     int sms, clusters[kSplitKinds];
+    int *status;
 };
 constexpr int kMaxDevices = 64;
 
 int ask_device(Device *d) {
     int dev = 0;
     int rc = record_cuda(cudaGetDevice(&dev));
+    if (!rc) rc = record_cuda(cudaGetSymbolAddress((void **)&d->status, default_status));
     if (!rc) rc = record_cuda(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev));
     for (const void *k : {(const void *)tile_kernel, (const void *)pair_kernel<SVDCACHE_F32, 128>, (const void *)pair_kernel<SVDCACHE_F32, 192>,
                           (const void *)pair_kernel<SVDCACHE_BF16, 128>, (const void *)pair_kernel<SVDCACHE_BF16, 192>,
@@ -956,6 +962,13 @@ TilePlan plan_tile(const GemmFp8Args &a, const Device &d) {
 }
 
 }  // namespace
+
+int gemm_fp8_status_word(int **word) {
+    Device d;
+    const int rc = device(&d);
+    if (!rc) *word = d.status;
+    return rc;
+}
 
 int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
     Device d;

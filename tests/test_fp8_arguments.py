@@ -70,3 +70,42 @@ def test_the_format_s_own_types_are_taken(small):
     assert torch.equal(q, a) and torch.equal(s, sa)
     sc.svdcache_gemm_fp8(q.view(v), s.view(e), b.view(v), sb.view(e), 128, D)
     assert torch.equal(C, D)
+
+
+FIRST_IN_A_CAPTURE = """
+import torch
+from paper_2601_07396_b200 import binding as sc
+x, w = torch.ones(40, 2048, device="cuda"), torch.ones(64, 2048, device="cuda")
+(a, sa), (b, sb) = sc.new_fp8(40, 2048), sc.new_fp8(64, 2048)
+C = torch.zeros(40, 64, device="cuda")
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    sc.svdcache_quantize_fp8(w, b, sb, tile_rows=128)
+    sc.svdcache_residual_rmsnorm_fp8(x, None, None, None, 0.0, a, sa)
+    sc.svdcache_gemm_fp8(a, sa, b, sb, 2048, C)
+assert float(C.abs().max()) == 0.0              # captured, not run
+graph.replay()
+torch.cuda.synchronize()
+assert bool((C == 2048.0).all()), C
+assert sc.gemm_status() == 0
+print("first calls captured")
+"""
+
+
+@gpu
+def test_a_process_may_begin_with_captured_calls():
+    r = subprocess.run([sys.executable, "-c", FIRST_IN_A_CAPTURE], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "first calls captured" in r.stdout, r.stdout + r.stderr
+
+
+@gpu
+def test_the_default_status_word_is_the_library_s_own():
+    word = sc.svdcache_gemm_fp8_status_word()
+    assert word and word % 4 == 0 and word == sc.svdcache_gemm_fp8_status_word()
+    assert sc.gemm_status() == sc.gemm_status("cuda:0") == sc.gemm_status(torch.device("cuda", 0)) == 0
+
+
+def test_status_entries_refuse():
+    assert sc.lib().svdcache_gemm_fp8_status_word(None) == -1
+    assert sc.lib().svdcache_gemm_fp8_status_query(None) == -1
