@@ -482,10 +482,9 @@ def svdcache_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: to
                       S_out: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
                       status: Optional[torch.Tensor] = None, stream=None) -> None:
     """C [M, N] = act(A B^T + bias) of the 8-bit matrices A [M, >= K] and B [N, >= K].  C is fp32 or bf16, or bytes
-    (uint8, float8_e4m3fn) with scales S_out.  `status`: one int32 on the device that receives a time-out; by default
-    the library's own on that device, which gemm_status() reads."""
-    word = None if status is None else status.data_ptr()
-    rc = (_calls or calls()).gemm(A, SA, B, SB, K, C, S_out, bias, act, word, None if stream is None else stream.cuda_stream)
+    (uint8, float8_e4m3fn) with scales S_out.  `status`: an int32 tensor on the device, whose first element
+    receives a time-out; by default the library's own on that device, which gemm_status() reads."""
+    rc = (_calls or calls()).gemm(A, SA, B, SB, K, C, S_out, bias, act, status, None if stream is None else stream.cuda_stream)
     if rc:
         raise SvdCacheError(rc, "gemm_fp8")
 

@@ -79,6 +79,15 @@ const float *vector(PyObject *o, int64_t n, int device, const char *what) {
     return static_cast<const float *>(t.data_ptr());
 }
 
+// where a time-out is written: nothing else may lie there
+int32_t *status_word(PyObject *o, int device) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, "status");
+    if (t.scalar_type() != at::kInt || t.numel() < 1 || !t.is_cuda() || t.get_device() != device)
+        refuse("status", "an int32 word on the same device is expected");
+    return static_cast<int32_t *>(t.data_ptr());
+}
+
 int plain_type(const at::Tensor &t, const char *what) {
     if (t.scalar_type() == at::kFloat) return SVDCACHE_F32;
     if (t.scalar_type() == at::kBFloat16) return SVDCACHE_BF16;
@@ -179,7 +188,7 @@ PyObject *norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// gemm(A, SA, B, SB, K, C, S_out or None, bias or None, act, address of the status word or None: the library's own, stream)
+// gemm(A, SA, B, SB, K, C, S_out or None, bias or None, act, status word or None: the library's own, stream)
 PyObject *gemm(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 11, [&] {
         const at::Tensor &c = tensor(a[5], "C");
@@ -197,7 +206,7 @@ PyObject *gemm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         } else {
             out = plain_type(c, "C");
         }
-        int32_t *status = a[9] == Py_None ? nullptr : reinterpret_cast<int32_t *>(static_cast<uintptr_t>(number(a[9])));
+        int32_t *status = status_word(a[9], dev);
         void *stream = stream_of(a[10], dev);
         return call(dev, [&] {
             const int rc = status ? SVDCACHE_OK : g_status_word(&status);

@@ -109,3 +109,22 @@ def test_the_default_status_word_is_the_library_s_own():
 def test_status_entries_refuse():
     assert sc.lib().svdcache_gemm_fp8_status_word(None) == -1
     assert sc.lib().svdcache_gemm_fp8_status_query(None) == -1
+
+
+@gpu
+def test_status_words_that_are_none(small):
+    """A word on the host or of another type would be written by the kernel when a wait runs out."""
+    x, a, sa, b, sb = small
+    C = torch.zeros(4, 32, device=DEV)
+    before = sc.svdcache_kernel_launches()
+    for bad in (torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32).pin_memory(), torch.zeros(1, dtype=torch.int64, device=DEV),
+                torch.zeros(1, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int16, device=DEV)):
+        with pytest.raises(ValueError):
+            sc.svdcache_gemm_fp8(a, sa, b, sb, 128, C, status=bad)
+    with pytest.raises(TypeError):
+        sc.svdcache_gemm_fp8(a, sa, b, sb, 128, C, status=a.data_ptr())
+    assert sc.svdcache_kernel_launches() == before
+    word = torch.zeros(3, dtype=torch.int32, device=DEV)
+    sc.svdcache_gemm_fp8(a, sa, b, sb, 128, C, status=word[1:])
+    torch.cuda.synchronize()
+    assert word.tolist() == [0, 0, 0] and bool(C.isfinite().all())
