@@ -432,6 +432,8 @@ ACT_NONE, ACT_GELU = 0, 1
 
 def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
     out = ctypes.c_size_t(0)
+    if not (0 <= rows < 1 << 31 and 0 <= cols < 1 << 31):   # ctypes would cut them to their low bits
+        raise SvdCacheError(-2, "fp8_scale_bytes")
     _check(lib().svdcache_fp8_scale_bytes(rows, cols, ctypes.byref(out)), "fp8_scale_bytes")
     return out.value
 

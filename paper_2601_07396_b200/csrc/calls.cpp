@@ -5,6 +5,8 @@
 // public functions, loads this module next to the library and hands it the library's entry points.
 #include <Python.h>
 
+#include <cstdint>
+
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -99,7 +101,8 @@ int device_of(const at::Tensor &t, const char *what) {
     return (int)t.get_device();
 }
 
-int dim32(int64_t n) { return n > 0x7FFFFFFF ? 0x7FFFFFFF : (int)n; }   // the library refuses what is that wide
+// a number beyond int becomes its nearest, which the library refuses wherever an int is expected here
+int dim32(int64_t n) { return n > INT32_MAX ? INT32_MAX : n < INT32_MIN ? INT32_MIN : (int)n; }
 
 long long number(PyObject *o) {
     const long long v = PyLong_AsLongLong(o);

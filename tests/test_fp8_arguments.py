@@ -128,3 +128,25 @@ def test_status_words_that_are_none(small):
     sc.svdcache_gemm_fp8(a, sa, b, sb, 128, C, status=word[1:])
     torch.cuda.synchronize()
     assert word.tolist() == [0, 0, 0] and bool(C.isfinite().all())
+
+
+@gpu
+def test_whole_numbers_are_not_cut(small):
+    """Arguments that would be in order modulo 2^32."""
+    x, a, sa, b, sb = small
+    C = torch.zeros(4, 32, device=DEV)
+    before = sc.svdcache_kernel_launches()
+    for wrap in (1 << 32, -(1 << 32)):
+        with pytest.raises(sc.SvdCacheError):
+            sc.svdcache_quantize_fp8(x, a, sa, tile_rows=1 + wrap)
+        with pytest.raises(sc.SvdCacheError):
+            sc.svdcache_gemm_fp8(a, sa, b, sb, 128, C, act=sc.ACT_GELU + wrap)
+        with pytest.raises(ValueError):
+            sc.svdcache_gemm_fp8(a, sa, b, sb, 128 + wrap, C)
+    assert sc.svdcache_kernel_launches() == before
+
+
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 32) + 8), ((1 << 64) + 1, 8), (-(1 << 64) + 1, 8), (1, -(1 << 32) + 8)])
+def test_sizes_are_not_cut(rows, cols):
+    with pytest.raises(sc.SvdCacheError):
+        sc.svdcache_fp8_scale_bytes(rows, cols)
