@@ -1,6 +1,6 @@
 """Thin ctypes binding of ``libsvdcache.so``: same names as ``include/svdcache.h``,
 argument marshalling only (tensor -> raw pointer, current stream -> void*; for the 8-bit calls
-by the extension ``_calls.so``).  Every step
+by the extension ``_calls.*.so``).  Every step
 of the path runs in the library's CUDA kernels; nothing here computes, and there is no
 fallback: a missing library or a failing call raises.
 """
@@ -13,6 +13,8 @@ import os
 from typing import Optional, Tuple
 
 import torch
+
+from .build import calls_path
 
 F32, BF16, FP8 = 0, 1, 2
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -442,7 +444,6 @@ def svdcache_fp8_scale_bytes(rows: int, cols: int) -> int:
 # checked by a small extension (csrc/calls.cpp), which calls the same C entry points.  It raises ValueError for
 # arguments that the C ABI cannot see to be wrong (types, shapes against one another, device, contiguity).  The values of an
 # 8-bit matrix are uint8 or float8_e4m3fn tensors, its scales uint8 or float8_e8m0fnu.
-CALLS_PATH = os.path.join(_HERE, "_calls.so")
 _calls = None
 
 
@@ -450,9 +451,10 @@ def calls():
     """Load the extension (once) and bind it to the library.  Raises if it has not been built."""
     global _calls
     if _calls is None:
-        if not os.path.exists(CALLS_PATH):
-            raise RuntimeError(f"{CALLS_PATH} is missing: build it with `python -m paper_2601_07396_b200.build`")
-        loader = importlib.machinery.ExtensionFileLoader("_calls", CALLS_PATH)
+        path = calls_path()
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2601_07396_b200.build`")
+        loader = importlib.machinery.ExtensionFileLoader("_calls", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
         L = lib()

@@ -1,5 +1,6 @@
-"""Builds ``libsvdcache.so`` (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and ``_calls.so`` (the argument side
-of the 8-bit calls, a Python extension over torch's tensors) with the host compiler."""
+"""Builds, in-tree, ``libsvdcache.so`` (the C-ABI CUDA library) with nvcc for sm_100a, and ``_calls.*.so`` (the argument side
+of the 8-bit calls, a Python extension over torch's tensors) with the host compiler.  The library needs neither the other
+nor torch."""
 from __future__ import annotations
 
 import glob
@@ -12,7 +13,6 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsvdcache.so")
 CALLS_SOURCE = os.path.join(CSRC, "calls.cpp")
-CALLS = os.path.join(HERE, "_calls.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -33,27 +33,33 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def calls_path() -> str:
+    """The extension for this interpreter and this torch: its name says both, so that one built with others is not loaded."""
+    import torch
+    return os.path.join(HERE, f"_calls.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so")
+
+
 def build_calls(force: bool = False) -> str:
     """Compile csrc/calls.cpp into the extension.  Returns its path."""
+    path = calls_path()
     deps = [CALLS_SOURCE, os.path.join(HERE, "..", "include", "svdcache.h")]
-    if not force and os.path.exists(CALLS) and all(os.path.getmtime(d) <= os.path.getmtime(CALLS) for d in deps):
-        return CALLS
+    if not force and os.path.exists(path) and all(os.path.getmtime(d) <= os.path.getmtime(path) for d in deps):
+        return path
     import torch
     from torch.utils import cpp_extension
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     include = [sysconfig.get_paths()["include"], *cpp_extension.include_paths(), os.path.join(cuda, "include")]
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
-    tmp = CALLS + f".tmp{os.getpid()}"
+    tmp = path + f".tmp{os.getpid()}"
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for d in include for a in ("-isystem", d)],
                     CALLS_SOURCE, "-o", tmp, f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
-    os.replace(tmp, CALLS)
-    return CALLS
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared object, and the extension.  Returns the library's path."""
-    build_calls(force)
+    """Compile every .cu under csrc/ into one shared object.  Returns its path."""
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -80,3 +86,4 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_calls(force="--force" in sys.argv))
