@@ -399,6 +399,20 @@ SVDCACHE_API int svdcache_last_path(void);
  * and svdcache_state_reset clears both.  Asynchronous on `stream`.  Nothing is faulted or hung. */
 SVDCACHE_API int svdcache_selftest_wait_timeout(void *state, int64_t limit_cycles, void *stream);
 
+/* How the 8-bit product is taken, for tests and benchmarks.  svdcache_gemm_fp8 chooses among two kernels and their tiles by a
+ * model of their times; plan (host, four words) names a choice:
+ *   {1, 128, 192 or 256, 2}            pairs of CTAs on tiles of 256 rows x that many columns (192: F32, BF16; 256: FP8)
+ *   {0, 16, 32, 64 or 128, 1 .. 8}     tiles of so many rows x 128 columns, K shared by 1, 2, 3, 4, 6 or 8 CTAs
+ * svdcache_gemm_fp8_plan tells the model's on the current device, and in the fourth word how many tiles follow one another on
+ * an SM at most.  svdcache_selftest_gemm_fp8 is svdcache_gemm_fp8 by the given plan (three words);
+ * SVDCACHE_ERR_INVALID_ARG if it is not one that the model may choose for such a product: tiles of the fewest rows that
+ * hold M, of 64 or 128 above that; several CTAs only where all clusters run at the same time, with two groups of K each. */
+SVDCACHE_API int svdcache_gemm_fp8_plan(int64_t M, int N, int K, int64_t lda, int64_t ldb, int out_dtype, int32_t *plan /* host, out */);
+SVDCACHE_API int svdcache_selftest_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb,
+                               const void *SB, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
+                               void *SC, int64_t M, int N, int K, int32_t *status, const int32_t *plan /* host */,
+                               void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -480,10 +480,9 @@ int svdcache_residual_rmsnorm_fp8(const void *H, int64_t ldh, const void *X, int
     return rmsnorm_fp8_launch(H, ldh, X, ldx, H_out, ldo, weight, eps, Q, ldq, S, rows, D, dtype, (cudaStream_t)stream);
 }
 
-int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
-                      const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
-                      int32_t *status, void *stream) {
-    NvtxRange range("svdcache_gemm_fp8");
+// every check of a product's arguments; args is filled where there is something to launch (M > 0)
+static int check_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB, const float *bias, int act,
+                          void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K, int32_t *status, GemmFp8Args *args) {
     if (act != SVDCACHE_ACT_NONE && act != SVDCACHE_ACT_GELU) return SVDCACHE_ERR_INVALID_ARG;
     if (out_dtype != SVDCACHE_F32 && out_dtype != SVDCACHE_BF16 && out_dtype != SVDCACHE_FP8) return SVDCACHE_ERR_INVALID_ARG;
     int rc = check_fp8_shape(M, K);
@@ -494,11 +493,45 @@ int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B,
     rc = check_fp8_matrix(A, lda, K, SA);
     if (!rc) rc = check_fp8_matrix(B, ldb, K, SB);
     if (!rc) rc = out_dtype == SVDCACHE_FP8 ? check_fp8_matrix(C, ldc, N, SC) : check_matrix(C, ldc, N, (int)elem_bytes(out_dtype));
-    if (rc) return rc;
     GemmFp8Args a{};
     a.A = A; a.B = B; a.SA = SA; a.SB = SB; a.lda = lda; a.ldb = ldb; a.ldc = ldc; a.bias = bias; a.C = C; a.SC = SC;
     a.M = M; a.N = N; a.K = K; a.act = act; a.out = out_dtype; a.status = status;
-    return gemm_fp8_launch(a, (cudaStream_t)stream);
+    *args = a;
+    return rc;
+}
+
+int svdcache_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
+                      const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
+                      int32_t *status, void *stream) {
+    NvtxRange range("svdcache_gemm_fp8");
+    GemmFp8Args a;
+    const int rc = check_gemm_fp8(A, lda, SA, B, ldb, SB, bias, act, C, ldc, out_dtype, SC, M, N, K, status, &a);
+    return rc || M == 0 ? rc : gemm_fp8_launch(a, nullptr, (cudaStream_t)stream);
+}
+
+int svdcache_gemm_fp8_plan(int64_t M, int N, int K, int64_t lda, int64_t ldb, int out_dtype, int32_t *plan) {
+    if (!plan || (out_dtype != SVDCACHE_F32 && out_dtype != SVDCACHE_BF16 && out_dtype != SVDCACHE_FP8)) return SVDCACHE_ERR_INVALID_ARG;
+    int rc = check_fp8_shape(M, K);
+    if (!rc) rc = check_fp8_shape(M, N);
+    if (rc) return rc;
+    if (M == 0 || lda < K || ldb < K) return SVDCACHE_ERR_BAD_SHAPE;
+    GemmFp8Args a{};
+    a.M = M; a.N = N; a.K = K; a.lda = lda; a.ldb = ldb; a.out = out_dtype;
+    GemmFp8Plan p{};
+    rc = gemm_fp8_plan(a, &p);
+    if (rc) return rc;
+    plan[0] = p.pairs; plan[1] = p.size; plan[2] = p.splits; plan[3] = (int32_t)(p.rounds < 0x7FFFFFFF ? p.rounds : 0x7FFFFFFF);
+    return SVDCACHE_OK;
+}
+
+int svdcache_selftest_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
+                               const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
+                               int32_t *status, const int32_t *plan, void *stream) {
+    if (!plan) return SVDCACHE_ERR_INVALID_ARG;
+    GemmFp8Args a;
+    const int rc = check_gemm_fp8(A, lda, SA, B, ldb, SB, bias, act, C, ldc, out_dtype, SC, M, N, K, status, &a);
+    const GemmFp8Plan p{plan[0] != 0, plan[1], plan[2], 0, 0};
+    return rc || M == 0 ? rc : gemm_fp8_launch(a, &p, (cudaStream_t)stream);
 }
 
 int svdcache_gemm_fp8_status_word(int32_t **word) {

@@ -142,7 +142,15 @@ struct GemmFp8Args {
     int act, out;           // SVDCACHE_ACT_*, dtype of C
     int *status;            // device word that receives SVDCACHE_ERR_TIMEOUT if a bounded wait runs out
 };
-int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s);
+// How a product is taken: by pairs of CTAs in tiles of 256 x `size`, or in tiles of `size` rows x 128 that `splits` CTAs
+// share; tiles that follow one another on an SM (at most), and the model's time.
+struct GemmFp8Plan {
+    bool pairs;
+    int size, splits;
+    int64_t rounds, time;
+};
+int gemm_fp8_plan(const GemmFp8Args &a, GemmFp8Plan *plan);        // the one that the model chooses (A, B, C and status are not used)
+int gemm_fp8_launch(const GemmFp8Args &a, const GemmFp8Plan *plan, cudaStream_t s);   // plan null: the model's; else one that it may choose
 int gemm_fp8_status_word(int **word);   // the current device's default status word
 
 }  // namespace svdc

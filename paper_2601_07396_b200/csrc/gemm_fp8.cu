@@ -819,20 +819,15 @@ int device(Device *d) {
     return rc;
 }
 
-// How tile_kernel would take a product.
-struct TilePlan {
-    int tile_m, splits, n_tiles, groups;
-    int64_t tiles, time;
-};
-
-int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
+int tile_launch(const GemmFp8Args &a, int tile_m, int splits, cudaStream_t s) {
     TileParams p{};
     p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
     p.act = a.act; p.out = a.out; p.status = a.status;
-    p.groups = t.groups; p.splits = t.splits; p.n_tiles = t.n_tiles; p.tile_m = t.tile_m;
+    p.groups = (int)fp8_groups(a.K); p.splits = splits; p.n_tiles = (a.N + kTileN - 1) / kTileN; p.tile_m = tile_m;
+    const int64_t tiles = (a.M + tile_m - 1) / tile_m * p.n_tiles;
     p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
-    if (t.tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    if (tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
     p.stage_bytes = kBBytes + p.a_bytes + 1024u;
     p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
@@ -850,7 +845,7 @@ int tile_launch(const GemmFp8Args &a, const TilePlan &t, cudaStream_t s) {
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
     if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, kTileN);
     if (rc) return rc;
-    return launch_early(tile_kernel, dim3((unsigned)(t.tiles * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p);
+    return launch_early(tile_kernel, dim3((unsigned)(tiles * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p);
 }
 
 // a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
@@ -912,6 +907,16 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
                         tm_sb, tm_c, p);
 }
 
+// Rows of tile_kernel's tiles: what M needs, up to 64 or 128.  (Fewer only where M has no more: an MMA's scale words begin at
+// an even column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
+int least_tile_rows(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : 64; }
+int most_tile_rows(int64_t M) { return M <= 64 ? least_tile_rows(M) : 128; }
+
+// Whether kSplits[i] CTAs may share a tile: all clusters run at the same time and each CTA has two groups of K.
+bool split_allowed(int64_t tiles, int groups, const Device &d, int i) {
+    return d.clusters[i] > 0 && (i == 0 || (tiles <= d.clusters[i] && groups >= 2 * kSplits[i]));
+}
+
 // Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4000,
 // N from 128 to 18432, K from 100 to 9216; over 698 shapes the choice takes 1-2 % more than the best of all on average and
 // up to a fifth at a few):
@@ -923,42 +928,56 @@ template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, c
 //               B's bytes at 5.6 TB/s, where that is more
 // N = 500, K = 100, M = 40: 3.9 us by pairs, 3.8 by small tiles.  N = 500, K = 9000, M = 1 / 40 / 512: 15.0 / 17.7 / 24.3 and
 // 6.2 / 7.4 / 11.2.  N = 18432, K = 3072, M = 1 / 40 / 256: 27.0 / 21.7 / 16.8 and 12.0 / 12.8 / 24.4.
-struct PairPlan {
-    int bn;
-    int64_t time;
-};
-
-PairPlan plan_pair(const GemmFp8Args &a, const Device &d) {
+GemmFp8Plan plan_pair(const GemmFp8Args &a, const Device &d) {
     const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, groups = fp8_groups(a.K), clusters = d.sms / 2;
     const int64_t fifths = (a.lda | a.ldb) % 128 ? 7 : 5;
-    auto time = [&](int bn, int64_t group) {
+    auto plan = [&](int bn, int64_t group) {
         const int64_t rounds = (m_tiles * ((a.N + bn - 1) / bn) + clusters - 1) / clusters, work = rounds * (40 + groups * group * fifths / 5);
-        return std::max(310 + work, 400 + (int64_t)a.N * a.K / 40000 + work / 16);   // the last term: fewer rounds where memory decides
+        // the last term: fewer rounds where memory decides
+        return GemmFp8Plan{true, bn, 2, rounds, std::max(310 + work, 400 + (int64_t)a.N * a.K / 40000 + work / 16)};
     };
-    const int wide = a.out == SVDCACHE_FP8 ? 256 : 192;
-    const int64_t t_wide = time(wide, wide == 256 ? 35 : 23), t_128 = time(128, 20);
-    return t_wide < t_128 ? PairPlan{wide, t_wide} : PairPlan{128, t_128};
+    const GemmFp8Plan wide = a.out == SVDCACHE_FP8 ? plan(256, 35) : plan(192, 23), narrow = plan(128, 20);
+    return wide.time < narrow.time ? wide : narrow;
 }
 
-TilePlan plan_tile(const GemmFp8Args &a, const Device &d) {
-    TilePlan best{};
+GemmFp8Plan plan_tile(const GemmFp8Args &a, const Device &d) {
+    GemmFp8Plan best{};
     const int groups = (int)fp8_groups(a.K), n_tiles = (a.N + kTileN - 1) / kTileN;
-    // Rows per tile: what M needs, up to 64 or 128.  (Fewer only where M has no more: an MMA's scale words begin at an even
-    // column of tensor memory, 32 rows each, so a tile begins at a multiple of 64.)
-    const int least = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64, most = a.M <= 64 ? least : 128;
-    for (int tile_m = least; tile_m <= most; tile_m *= 2) {
+    for (int tile_m = least_tile_rows(a.M); tile_m <= most_tile_rows(a.M); tile_m *= 2) {
         const int64_t tiles = (a.M + tile_m - 1) / tile_m * n_tiles;
-        // CTAs per tile: such that all clusters run at the same time and each CTA has two groups of K
         for (int i = 0; i < kSplitKinds; ++i) {
             const int splits = kSplits[i], fit = d.clusters[i];
-            if (i > 0 && (tiles > fit || groups < 2 * splits)) break;
+            if (!split_allowed(tiles, groups, d, i)) continue;
             const int own = (tile_m + splits - 1) / splits, each = (groups + splits - 1) / splits;
+            const int64_t rounds = (tiles + fit - 1) / fit;
             const int64_t ends = 210 + (splits > 1 ? 120 : 0) + tile_m * 3 / 2 + (a.out == SVDCACHE_FP8 ? own * 3 / 2 : own * 2 / 5);
-            const int64_t time = ends + std::max((tiles + fit - 1) / fit * each * (16 + tile_m / 4), (int64_t)a.N * a.K / 56000);
-            if (!best.splits || time < best.time) best = {tile_m, splits, n_tiles, groups, tiles, time};
+            const int64_t time = ends + std::max(rounds * each * (16 + tile_m / 4), (int64_t)a.N * a.K / 56000);
+            if (!best.splits || time < best.time) best = {false, tile_m, splits, rounds, time};
         }
     }
     return best;
+}
+
+GemmFp8Plan choose(const GemmFp8Args &a, const Device &d) {
+    const GemmFp8Plan t = plan_tile(a, d), p = plan_pair(a, d);
+    return t.splits > 0 && t.time < p.time ? t : p;
+}
+
+bool allowed(const GemmFp8Args &a, const GemmFp8Plan &plan, const Device &d) {
+    if (plan.pairs) return plan.splits == 2 && (plan.size == 128 || plan.size == (a.out == SVDCACHE_FP8 ? 256 : 192));
+    if (plan.size != least_tile_rows(a.M) && plan.size != most_tile_rows(a.M)) return false;
+    const int64_t tiles = (a.M + plan.size - 1) / plan.size * ((a.N + kTileN - 1) / kTileN);
+    for (int i = 0; i < kSplitKinds; ++i)
+        if (plan.splits == kSplits[i]) return split_allowed(tiles, (int)fp8_groups(a.K), d, i);
+    return false;
+}
+
+int run(const GemmFp8Args &a, const GemmFp8Plan &plan, const Device &d, cudaStream_t s) {
+    if (!plan.pairs) return tile_launch(a, plan.size, plan.splits, s);
+    const int clusters = d.sms / 2;
+    if (a.out == SVDCACHE_FP8) return plan.size == 256 ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
+    if (a.out == SVDCACHE_BF16) return plan.size == 192 ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
+    return plan.size == 192 ? pair_launch<SVDCACHE_F32, 192>(a, clusters, s) : pair_launch<SVDCACHE_F32, 128>(a, clusters, s);
 }
 
 }  // namespace
@@ -970,17 +989,19 @@ int gemm_fp8_status_word(int **word) {
     return rc;
 }
 
-int gemm_fp8_launch(const GemmFp8Args &a, cudaStream_t s) {
+int gemm_fp8_plan(const GemmFp8Args &a, GemmFp8Plan *plan) {
+    Device d;
+    const int rc = device(&d);
+    if (!rc) *plan = choose(a, d);
+    return rc;
+}
+
+int gemm_fp8_launch(const GemmFp8Args &a, const GemmFp8Plan *plan, cudaStream_t s) {
     Device d;
     const int rc = device(&d);
     if (rc) return rc;
-    const TilePlan t = plan_tile(a, d);
-    const PairPlan p = plan_pair(a, d);
-    if (t.time < p.time) return tile_launch(a, t, s);
-    const int clusters = d.sms / 2;
-    if (a.out == SVDCACHE_FP8) return p.bn == 256 ? pair_launch<SVDCACHE_FP8, 256>(a, clusters, s) : pair_launch<SVDCACHE_FP8, 128>(a, clusters, s);
-    if (a.out == SVDCACHE_BF16) return p.bn == 192 ? pair_launch<SVDCACHE_BF16, 192>(a, clusters, s) : pair_launch<SVDCACHE_BF16, 128>(a, clusters, s);
-    return p.bn == 192 ? pair_launch<SVDCACHE_F32, 192>(a, clusters, s) : pair_launch<SVDCACHE_F32, 128>(a, clusters, s);
+    if (plan && !allowed(a, *plan, d)) return SVDCACHE_ERR_INVALID_ARG;
+    return run(a, plan ? *plan : choose(a, d), d, s);
 }
 
 }  // namespace svdc

@@ -12,15 +12,15 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
-# one column tile or a few, and long sums: 2 to 8 CTAs per tile of 16, 32, 64 and 128 rows
-@pytest.mark.parametrize("M,N,K", [(1, 128, 9216), (11, 130, 1540), (31, 300, 4100), (64, 130, 6000), (100, 2100, 6000), (250, 400, 9000)])
-def test_shared_tiles_in_company(M, N, K):
+@pytest.mark.parametrize("M,N,K,plan", [(1, 128, 9216, (0, 16, 8)), (11, 130, 1540, (0, 16, 6)), (31, 300, 4100, (0, 32, 4)), (64, 130, 6000, (0, 64, 8)),
+                                        (64, 400, 6000, (0, 64, 2)), (100, 2100, 6000, (0, 128, 6)), (128, 900, 3000, (0, 128, 2)), (250, 400, 9000, (0, 64, 3))])
+def test_shared_tiles_in_company(M, N, K, plan):
     a, sa = random_fp8(M, K, 1)
     b, sb = random_fp8(N, K, 2, 128)
     pitch = -(-N // 16) * 16
 
     def product(C, S, stream=None):
-        sc.svdcache_gemm_fp8(a, sa, b, sb, K, C[:, :N], S_out=S, stream=stream)
+        sc.svdcache_selftest_gemm_fp8(a, sa, b, sb, K, C[:, :N], plan, S_out=S, stream=stream)
 
     want, want_s = sc.new_fp8(M, N)
     product(want, want_s)
