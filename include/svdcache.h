@@ -406,12 +406,14 @@ SVDCACHE_API int svdcache_selftest_wait_timeout(void *state, int64_t limit_cycle
  * svdcache_gemm_fp8_plan tells the model's on the current device, and in the fourth word how many tiles follow one another on
  * an SM at most.  svdcache_selftest_gemm_fp8 is svdcache_gemm_fp8 by the given plan (three words);
  * SVDCACHE_ERR_INVALID_ARG if it is not one that the model may choose for such a product: tiles of the fewest rows that
- * hold M, of 64 or 128 above that; several CTAs only where all clusters run at the same time, with two groups of K each. */
+ * hold M, of 64 or 128 above that; several CTAs only where all clusters run at the same time, with two groups of K each.
+ * limit_cycles 0: an ordinary product.  1 .. 2e8: a test of the time-out path: no operand is loaded, every wait runs out
+ * after so many SM cycles, the kernel returns with SVDCACHE_ERR_TIMEOUT in *status, and C holds nothing of use. */
 SVDCACHE_API int svdcache_gemm_fp8_plan(int64_t M, int N, int K, int64_t lda, int64_t ldb, int out_dtype, int32_t *plan /* host, out */);
 SVDCACHE_API int svdcache_selftest_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb,
                                const void *SB, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
                                void *SC, int64_t M, int N, int K, int32_t *status, const int32_t *plan /* host */,
-                               void *stream);
+                               int64_t limit_cycles, void *stream);
 
 #ifdef __cplusplus
 }

@@ -78,7 +78,7 @@ SIGNATURES = {
     "svdcache_gemm_fp8_status_query": (_ci, [ctypes.POINTER(ctypes.c_int32)]),
     "svdcache_gemm_fp8": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp]),
     "svdcache_gemm_fp8_plan": (_ci, [_i64, _ci, _ci, _i64, _i64, _ci, _vp]),
-    "svdcache_selftest_gemm_fp8": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp, _vp]),
+    "svdcache_selftest_gemm_fp8": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp, _i64, _vp]),
 }
 
 
@@ -506,16 +506,18 @@ def svdcache_gemm_fp8_plan(M: int, N: int, K: int, out: int, lda: Optional[int] 
 
 def svdcache_selftest_gemm_fp8(A: torch.Tensor, SA: torch.Tensor, B: torch.Tensor, SB: torch.Tensor, K: int, C: torch.Tensor, plan,
                                S_out: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
-                               status: Optional[torch.Tensor] = None, stream=None) -> None:
+                               status: Optional[torch.Tensor] = None, limit_cycles: int = 0, stream=None) -> None:
     """svdcache_gemm_fp8 by the given plan (pairs, size of the tiles, CTAs per tile), which has to be one that the product may
-    be taken by.  For tests: of the tensors only what the C ABI sees is checked."""
+    be taken by.  limit_cycles > 0: nothing is loaded and the kernel's waits run out after so many cycles.  For tests: of the
+    tensors only what the C ABI sees is checked."""
     (M, N), out = C.shape, _DTYPES.get(C.dtype, FP8)
     words = (ctypes.c_int32 * 3)(*plan[:3])
     pitch = lambda t: t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16  # noqa: E731
     with torch.cuda.device(C.device):
         word = _ptr(status) if status is not None else svdcache_gemm_fp8_status_word()
         _check(lib().svdcache_selftest_gemm_fp8(_ptr(A), pitch(A), _ptr(SA), _ptr(B), pitch(B), _ptr(SB), _ptr(bias), act, _ptr(C), pitch(C), out,
-                                                _ptr(S_out), M, N, K, word, words, _stream(stream)), "selftest_gemm_fp8")
+                                                _ptr(S_out), M, N, K, word, words, limit_cycles, _stream(stream)),
+               "selftest_gemm_fp8")
 
 
 def svdcache_gemm_fp8_status_word() -> int:

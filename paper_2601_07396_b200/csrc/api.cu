@@ -526,12 +526,14 @@ int svdcache_gemm_fp8_plan(int64_t M, int N, int K, int64_t lda, int64_t ldb, in
 
 int svdcache_selftest_gemm_fp8(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
                                const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
-                               int32_t *status, const int32_t *plan, void *stream) {
-    if (!plan) return SVDCACHE_ERR_INVALID_ARG;
+                               int32_t *status, const int32_t *plan, int64_t limit_cycles, void *stream) {
+    if (!plan || limit_cycles < 0 || limit_cycles > 200000000LL) return SVDCACHE_ERR_INVALID_ARG;   // at most ~0.1 s
     GemmFp8Args a;
     const int rc = check_gemm_fp8(A, lda, SA, B, ldb, SB, bias, act, C, ldc, out_dtype, SC, M, N, K, status, &a);
+    if (rc || M == 0) return rc;
     const GemmFp8Plan p{plan[0] != 0, plan[1], plan[2], 0, 0};
-    return rc || M == 0 ? rc : gemm_fp8_launch(a, &p, (cudaStream_t)stream);
+    a.limit = limit_cycles;
+    return gemm_fp8_launch(a, &p, (cudaStream_t)stream);
 }
 
 int svdcache_gemm_fp8_status_word(int32_t **word) {

@@ -141,6 +141,7 @@ struct GemmFp8Args {
     int N, K;
     int act, out;           // SVDCACHE_ACT_*, dtype of C
     int *status;            // device word that receives SVDCACHE_ERR_TIMEOUT if a bounded wait runs out
+    long long limit;        // 0, or for a test of that: cycles after which the waits run out, for loads that are not made
 };
 // How a product is taken: by pairs of CTAs in tiles of 256 x `size`, or in tiles of `size` rows x 128 that `splits` CTAs
 // share; tiles that follow one another on an SM (at most), and the model's time.

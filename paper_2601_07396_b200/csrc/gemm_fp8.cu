@@ -35,7 +35,7 @@ constexpr int kMaxStages = 12;
 
 struct TileParams {
     int64_t M, ldc;
-    int N, K, groups, splits, n_tiles, tile_m, stages, tmem_cols;
+    int N, groups, splits, n_tiles, tile_m, stages, tmem_cols;
     int64_t pieces;                 // scale pieces along K
     uint32_t a_bytes, stage_bytes;
     const uint8_t *SA, *SB;
@@ -45,7 +45,19 @@ struct TileParams {
     int64_t pieces_c;
     int act, out;
     int *status;
+    int limit, withhold;            // of every wait, in units of 1024 cycles; `withhold`: nothing is loaded, so that they run out
 };
+
+// A wait ran out: tell the host, and give what is in flight (loads, sums under way, MMAs) time to land before the memory
+// and the tensor memory go.  By all threads of a CTA.
+__device__ __forceinline__ void settle(int *status) {
+    if ((threadIdx.x & 31) == 0) {
+        atomicExch(status, SVDCACHE_ERR_TIMEOUT);
+        const long long t0 = clock64();
+        while (clock64() - t0 < kWaitCycles / 100) {}
+    }
+    __syncwarp();
+}
 
 // four neighbouring columns n .. n + 3 of row m of C (n a multiple of 4): plain types
 __device__ __forceinline__ void store_plain(const TileParams &p, int64_t m, int n, const float (&v)[4]) {
@@ -156,10 +168,10 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxStages + 2];
     __shared__ uint32_t tmem_slot_mem;
-    __shared__ int abort_mem;
+    __shared__ int control_mem[2];               // abort flag, limit of the waits
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxStages, done_bar = empty + 8 * kMaxStages, parts_bar = done_bar + 8;
-    volatile int *abort_flag = &abort_mem;
+    volatile int *control = control_mem;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
     const int S = p.splits;
@@ -168,6 +180,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const int n_tile = tile % p.n_tiles;
     const int64_t m0 = (int64_t)(tile / p.n_tiles) * p.tile_m;
     const int count = (p.groups - rank + S - 1) / S;                    // groups rank, rank + S, ... of K: at least one
+    const int loaded = p.withhold ? 0 : count;
     const int per = (p.tile_m + S - 1) / S, own = min(per, p.tile_m - rank * per);   // rows that a CTA finishes
     // the CTA's own sum goes where the ring was (all loads have been consumed by then); the parts that others send, behind
     // both
@@ -177,7 +190,8 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
         mbar_init(done_bar, 1);
         mbar_init(parts_bar, 1);
-        abort_mem = 0;
+        control_mem[0] = 0;
+        control_mem[1] = p.limit;
         fence_barrier_init();
         if (S > 1) mbar_arrive_expect_tx(parts_bar, (uint32_t)(S * own) * kTileN * 4u);   // this CTA's rows from all S of them
         prefetch_tensormap(&tm_a);
@@ -192,7 +206,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     // the empty ring is filled before anything else is set up; a piece of scales comes with every group that is the
     // CTA's first in it
     if (warp == 0 && elect_one())
-        for (int i = 0; i < p.stages && i < count; ++i)
+        for (int i = 0; i < p.stages && i < loaded; ++i)
             request_group(tm_a, tm_b, p, base + i * p.stage_bytes, full + 8 * i, rank + i * S, i == 0 || (rank + i * S) % kScaleGroups < S, m0, n_tile);
     tc_fence_before();
     __syncthreads();
@@ -210,8 +224,8 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         if (elect_one()) {
             int s = 0;
             uint32_t ph = 0;
-            for (int i = p.stages; i < count; ++i) {
-                if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) break;
+            for (int i = p.stages; i < loaded; ++i) {
+                if (!mbar_wait_control(empty + 8 * s, ph, control, 1)) break;
                 const int g = rank + i * S;
                 request_group(tm_a, tm_b, p, base + s * p.stage_bytes, full + 8 * s, g, g % kScaleGroups < S, m0, n_tile);
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
@@ -232,7 +246,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
 #pragma unroll 4
             for (int i = 0; i < count; ++i) {
                 const int g = rank + i * S;
-                if (!mbar_wait(full + 8 * s, ph, abort_flag, 2)) break;
+                if (!mbar_wait_control(full + 8 * s, ph, control, 2)) break;
                 tc_fence_after();
                 const uint32_t src = base + s * p.stage_bytes;
                 if (i == 0 || g % kScaleGroups < S) {
@@ -258,7 +272,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     if (S > 1) cluster_wait();                                          // the other CTAs' barriers exist
     if (warp >= 2) {
         const int q = warp & 3;
-        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(done_bar, 0u, abort_flag, 3));
+        const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait_control(done_bar, 0u, control, 3));
         tc_fence_after();
         for (int c = 0; ok && c < p.tile_m; c += 32) {
             uint32_t acc[32];
@@ -280,20 +294,12 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         }
     }
     __syncthreads();
+    if (control[0]) settle(p.status);
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
     }
-    if (S > 1 && !mbar_wait_cluster(parts_bar, 0u)) *abort_flag = 5;
-    if (*abort_flag) {
-        // a wait ran out: tell the host, and let what is in flight land before the memory goes
-        if (lane == 0) {
-            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
-            const long long t0 = clock64();
-            while (clock64() - t0 < kWaitCycles / 100) {}
-        }
-    }
-    __syncwarp();
+    if (S > 1 && !__all_sync(0xFFFFFFFFu, mbar_wait_cluster(parts_bar, 0u, control))) settle(p.status);
     if (S > 1) cluster_arrive();                                        // this CTA has all its parts (or has waited long enough)
     switch (S) {
         case 1: finish_rows<1, 4>(p, parts, rank, m0, n_tile, bias); break;
@@ -366,13 +372,14 @@ struct Divisor {
 struct PairParams {
     int64_t M, ldc;
     void *C;
-    int N, groups, m_tiles, n_tiles, tiles, bands;
+    int N, groups, tiles, bands;
     Divisor band_tiles, band_rows, last_rows;        // tiles of a band; tile rows of a band, of the last one
     const float *bias;
     uint8_t *SC;
     int64_t pieces_c;
     int act;
     int *status;
+    int limit, withhold;                             // as in TileParams
 };
 
 struct TileAt { int m, n; };
@@ -469,10 +476,10 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     __shared__ __align__(8) unsigned long long bar_mem[2 * kMaxPairStages + 4];
     __shared__ __align__(16) float bias_mem[8][T::kWarpCols];
     __shared__ uint32_t tmem_slot_mem;
-    __shared__ int abort_mem;
+    __shared__ int control_mem[2];               // abort flag, limit of the waits
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bar_mem), empty = full + 8 * kMaxPairStages, acc_full = empty + 8 * kMaxPairStages, acc_empty = acc_full + 16;
-    volatile int *abort_flag = &abort_mem;
+    volatile int *control = control_mem;
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x & 1u;           // in the cluster
     const int cluster = (int)(blockIdx.x >> 1), clusters = (int)(gridDim.x >> 1);
@@ -483,7 +490,8 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             mbar_init(acc_full + 8 * i, 1);
             mbar_init(acc_empty + 8 * i, kHalves ? 16 : 8);   // the epilogue warps of both CTAs that read it
         }
-        abort_mem = 0;
+        control_mem[0] = 0;
+        control_mem[1] = p.limit;
         fence_barrier_init();
         prefetch_tensormap(&tm_a);
         prefetch_tensormap(&tm_b);
@@ -504,7 +512,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
     const uint32_t tmem = *(volatile uint32_t *)&tmem_slot_mem;
 
     if (warp == 0) {
-        if (elect_one()) {
+        if (!p.withhold && elect_one()) {
             int s = 0;
             uint32_t ph = 1;
             for (int t = cluster; t < p.tiles; t += clusters) {
@@ -513,7 +521,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
                 // unrolled as tile_kernel's loop over groups is, here and in the issuer (256 x 3072 x 12288 22.6 -> 21.8 us)
 #pragma unroll 4
                 for (int g = 0; g < p.groups; ++g) {
-                    if (!mbar_wait(empty + 8 * s, ph, abort_flag, 1)) goto done;
+                    if (!mbar_wait_control(empty + 8 * s, ph, control, 1)) goto done;
                     const uint32_t dst = base + s * T::kStageBytes, bar = cluster_addr(full + 8 * s, 0);
                     const bool scales = (g & (kScaleGroups - 1)) == 0;
                     if (rank == 0)
@@ -540,16 +548,16 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             for (int t = cluster; t < p.tiles; t += clusters, ++it) {
                 const uint32_t b = it & 1u;
                 if (kHalves) {
-                    if (it > 0 && !mbar_wait(acc_empty, b ^ 1u, abort_flag, 2)) goto done;
+                    if (it > 0 && !mbar_wait_control(acc_empty, b ^ 1u, control, 2)) goto done;
                 } else {
-                    if (it > 1 && !mbar_wait(acc_empty + 8 * b, (it >> 1 & 1u) ^ 1u, abort_flag, 2)) goto done;
+                    if (it > 1 && !mbar_wait_control(acc_empty + 8 * b, (it >> 1 & 1u) ^ 1u, control, 2)) goto done;
                 }
                 tc_fence_after();
                 const uint32_t acc = tmem + b * T::kAccStep;
                 const uint32_t b_word = BN == 192 ? (uint32_t)(pair_tile(p, t).n & 1) * 2u : 0u;   // a tile of 192 may begin in the middle of a piece
 #pragma unroll 4
                 for (int g = 0; g < p.groups; ++g) {
-                    if (!mbar_wait(full + 8 * s, ph, abort_flag, 3)) goto done;
+                    if (!mbar_wait_control(full + 8 * s, ph, control, 3)) goto done;
                     tc_fence_after();
                     const uint32_t src = base + s * T::kStageBytes;
                     if ((g & (kScaleGroups - 1)) == 0) {
@@ -596,7 +604,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             for (int j = 0; j < kBlocks; ++j) bias[j * 32 + lane] = next_bias[j];
             __syncwarp();
             request_bias(t + (kHalves ? 1 : 2) * clusters);
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full + (kHalves ? 0 : 8 * group), (kHalves ? it : it >> 1) & 1u, abort_flag, 4))) goto done;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_control(acc_full + (kHalves ? 0 : 8 * group), (kHalves ? it : it >> 1) & 1u, control, 4))) goto done;
             tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (it & 1u) * T::kAccStep + (kHalves ? group * 128 : 0);
             // halves: the columns that the next accumulator shares are the last 32 of the first one and the first 32 of
@@ -706,15 +714,7 @@ pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
 done:
     __syncwarp();
     __syncthreads();
-    if (*abort_flag) {
-        // a wait ran out: tell the host, and let what is in flight land before the memory goes
-        if (threadIdx.x == 0) {
-            atomicExch(p.status, SVDCACHE_ERR_TIMEOUT);
-            const long long t0 = clock64();
-            while (clock64() - t0 < kWaitCycles / 100) {}
-        }
-        __syncthreads();
-    }
+    if (control[0]) settle(p.status);
     tc_fence_before();
     cluster_sync();      // neither CTA signals the other any more
     if (warp == 1) {
@@ -819,11 +819,14 @@ int device(Device *d) {
     return rc;
 }
 
+// in units of 1024 cycles
+int wait_limit(const GemmFp8Args &a) { return (int)((a.limit > 0 ? a.limit : kWaitCycles) / 1024); }
+
 int tile_launch(const GemmFp8Args &a, int tile_m, int splits, cudaStream_t s) {
     TileParams p{};
-    p.M = a.M; p.N = a.N; p.K = a.K; p.ldc = a.ldc;
+    p.M = a.M; p.N = a.N; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
-    p.act = a.act; p.out = a.out; p.status = a.status;
+    p.act = a.act; p.out = a.out; p.status = a.status; p.limit = wait_limit(a); p.withhold = a.limit > 0;
     p.groups = (int)fp8_groups(a.K); p.splits = splits; p.n_tiles = (a.N + kTileN - 1) / kTileN; p.tile_m = tile_m;
     const int64_t tiles = (a.M + tile_m - 1) / tile_m * p.n_tiles;
     p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
@@ -882,19 +885,20 @@ int out_map(CUtensorMap *m, const GemmFp8Args &a) {
 template <int OUT, int BN> int pair_launch(const GemmFp8Args &a, int clusters, cudaStream_t s) {
     PairParams p{};
     p.M = a.M; p.N = a.N; p.groups = (int)fp8_groups(a.K); p.C = a.C; p.ldc = a.ldc;
-    p.n_tiles = (a.N + BN - 1) / BN;
-    const int64_t m_tiles = (a.M + kPairM - 1) / kPairM;
-    if (m_tiles * p.n_tiles > 0x3FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-    p.m_tiles = (int)m_tiles;
-    p.tiles = p.m_tiles * p.n_tiles;
+    const int n_tiles = (a.N + BN - 1) / BN;
+    const int64_t tiles = (a.M + kPairM - 1) / kPairM * n_tiles;
+    if (tiles > 0x3FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    const int m_tiles = (int)((a.M + kPairM - 1) / kPairM);
+    p.tiles = (int)tiles;
     const int64_t fit = kBandBytes / ((int64_t)kPairM * a.K), most = fit < 4 ? 4 : fit > kBandRows ? kBandRows : fit;
-    const int bands = (int)((p.m_tiles + most - 1) / most);
-    const int rows = (p.m_tiles + bands - 1) / bands;
-    p.bands = (p.m_tiles + rows - 1) / rows;
-    p.band_tiles = Divisor::of(rows * p.n_tiles);
+    const int bands = (int)((m_tiles + most - 1) / most);
+    const int rows = (m_tiles + bands - 1) / bands;
+    p.bands = (m_tiles + rows - 1) / rows;
+    p.band_tiles = Divisor::of(rows * n_tiles);
     p.band_rows = Divisor::of(rows);
-    p.last_rows = Divisor::of(p.m_tiles - (p.bands - 1) * rows);
+    p.last_rows = Divisor::of(m_tiles - (p.bands - 1) * rows);
     p.bias = a.bias; p.SC = (uint8_t *)a.SC; p.pieces_c = fp8_piece_cols(a.N); p.act = a.act; p.status = a.status;
+    p.limit = wait_limit(a); p.withhold = a.limit > 0;
     CUtensorMap tm_a, tm_b, tm_sa, tm_sb, tm_c;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, 128);
     if (!rc) rc = byte_map(&tm_b, a.B, a.N, a.K, a.ldb, BN / 2);

@@ -106,6 +106,23 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// The same for kernels whose limit a test sets: beside the abort flag control[0], in shared memory, control[1] holds it in units
+// of 1024 cycles, read only where a wait is long.
+__device__ __forceinline__ bool mbar_wait_control(uint32_t bar, uint32_t parity, volatile int *control, int site) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 0u) {
+            if (control[0]) return false;
+            if (clock64() - t0 > control[1] * 1024LL) {
+                atomicCAS(const_cast<int *>(control), 0, site);
+                return false;
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------ TMA ---
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *m) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
@@ -200,8 +217,9 @@ __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Bounded wait for what other CTAs of the cluster send to this one's shared memory.  It does not give up when
-// another thread has: whoever else holds this CTA's addresses must be done with them before the CTA leaves.
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
+// another thread has: whoever else holds this CTA's addresses must be done with them before the CTA leaves.  Its limit is
+// twice that of control[1], since the others may have waited before they sent.
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *control) {
     const long long t0 = clock64();
     for (uint32_t it = 0;; ++it) {
         uint32_t ok;
@@ -215,7 +233,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
             : "r"(bar), "r"(parity)
             : "memory");
         if (ok) return true;
-        if ((it & 63u) == 63u && clock64() - t0 > 2 * kWaitCycles) return false;
+        if ((it & 63u) == 63u && clock64() - t0 > control[1] * 2048LL) return false;
     }
 }
 

@@ -124,5 +124,5 @@ def test_plan_entries_refuse():
     assert ask(M=0) == -2 and ask(M=-1) == -2 and ask(N=0) == -2 and ask(K=131073) == -2 and ask(lda=99) == -2 and ask(ldb=99) == -2
     P = 1 << 20      # nothing reads it
     args = [P, 112, P, P, 112, P, None, 0, P, 64, 1, None, 4, 64, 100, P]
-    assert L.svdcache_selftest_gemm_fp8(*args, None, None) == -1
-    assert L.svdcache_selftest_gemm_fp8(*args[:1], 104, *args[2:], plan, None) == -3
+    assert L.svdcache_selftest_gemm_fp8(*args, None, 0, None) == -1
+    assert L.svdcache_selftest_gemm_fp8(*args[:1], 104, *args[2:], plan, 0, None) == -3
