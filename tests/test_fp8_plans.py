@@ -80,6 +80,25 @@ def test_pairs_in_several_rounds(M, N, K, out, bn):
 
 
 @gpu
+@pytest.mark.parametrize("act", [sc.ACT_NONE, sc.ACT_GELU])
+@pytest.mark.parametrize("M,N,K,plan", [(3, 300, 1540, (0, 16, 1)), (40, 300, 1540, (0, 64, 3)), (200, 300, 2100, (0, 128, 8)), (300, 300, 200, (1, 128, 2)),
+                                        (300, 300, 200, (1, 256, 2))])
+def test_infinities_in_an_8_bit_output(M, N, K, plan, act):
+    """Inf and NaN become the NaN code and stay with their element; their group's scale is that of its finite values."""
+    a, sa = random_fp8(M, K, 1)
+    b, sb = random_fp8(N, K, 2, 128)
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(1))
+    bias[5], bias[130], bias[131], bias[299] = float("inf"), float("-inf"), float("nan"), float("inf")
+    bias = bias.to(DEV)
+    with np.errstate(invalid="ignore"):
+        y, err = product64(a, sa, b, sb, M, N, K, bias, act)
+    q, s = junk_fp8(M, N)
+    sc.svdcache_selftest_gemm_fp8(a, sa, b, sb, K, q[:, :N], plan, S_out=s, bias=bias, act=act)
+    check_near(q, s, y, err)
+    check_padding(q, s, M, N)
+
+
+@gpu
 @pytest.mark.parametrize("M,N,K,out", [(1, 640, 4096, "bf16"), (24, 6724, 9381, "bf16"), (100, 2100, 6000, "fp8"), (959, 7366, 3318, "f32"),
                                        (2048, 1152, 1152, "fp8"), (40, 512, 100, "bf16")])
 def test_a_product_is_taken_by_the_plan_that_is_told(M, N, K, out):
