@@ -326,8 +326,10 @@ SVDCACHE_API int svdcache_left_factors(const float *C, const double *sigma, int6
 /* ---------------------------------------------------------------------------------
  * The 8-bit linear path around a cached block (no counterpart in the paper's equations; its
  * Table 3 pairs the method with an 8-bit quantised model).  A full step needs the block's
- * feature F from the network's own linear layers, and a cached step's Fhat is added to the
- * residual stream before the next block's norm: these calls are those two neighbours.
+ * feature F from the network's own linear layers: the quantiser and the product are these in 8 bits, for
+ * any block.  The norm is what follows F or Fhat in models that add a block's feature to the residual
+ * stream as it is and begin the next block with an RMS norm; it has no gate, shift or mean, so blocks with
+ * a gated addition and a modulated layer norm form their norm's output themselves and quantise it.
  *
  * 8-bit matrix: rows of e4m3 values (one byte each, pitch ld in bytes) and a scale buffer.
  *   - Every 1 x 128 group of a row has one scale, a power of two 2^e held as the byte e + 127
@@ -349,11 +351,16 @@ SVDCACHE_API int svdcache_left_factors(const float *C, const double *sigma, int6
  *              Q, S = y in 8 bits, a scale per 1 x 128 group.  fp32 arithmetic, y from the unrounded
  *              h.  X may be NULL (plain norm), H_out NULL (h not kept) or H itself (in place),
  *              weight (device, D fp32) NULL for ones.  Needs 8 <= D <= 16384, D % 8 == 0, eps >= 0.
+ *              The sum of squares is fp32 as well: where it exceeds that type (one element of 1.8e19 is enough)
+ *              the row's finite values become 0, and squares below 1e-45 count as 0 (which matters where eps is
+ *              as small).
  *   svdcache_gemm_fp8       C = act(A B^T + bias): A (M x K) and B (N x K) 8-bit with scales SA and
  *              SB, bias device N fp32 or NULL, act SVDCACHE_ACT_NONE or SVDCACHE_ACT_GELU (tanh
  *              form).  C (M x N, pitch ldc in ELEMENTS) is F32, BF16 or FP8; FP8 writes its scales
- *              (a scale per 1 x 128 group) to SC, which is ignored otherwise.  Products are exact,
- *              sums fp32 in the tensor cores.  1 <= N, K <= 131072.
+ *              (a scale per 1 x 128 group) to SC, which is ignored otherwise.  Products are exact; sums are
+ *              the tensor cores' fp32, which truncates: off by 3e-7 of the result at K = 3072, 1.5e-6 at 12288
+ *              (2-norm; an fp32 library product: 1e-7, 2e-7).  gelu adds less than 2^-17 of its value.
+ *              1 <= N, K <= 131072.
  *              status (device, one int32 that the caller sets to 0 once) receives
  *              SVDCACHE_ERR_TIMEOUT if a bounded in-kernel wait runs out; it is never cleared here.
  *   svdcache_gemm_fp8_status_word   the address of a status word that the library itself has on the

@@ -6,8 +6,8 @@
 // 128 rows x 4 groups reaches tensor memory as it is stored (tcgen05.cp), one word per row whose byte g % 4 the
 // four MMAs of group g name.  Sums are fp32 in tensor memory.
 //
-// tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns are up to 128 rows of
-// C, so that few rows of C waste no tensor work.  One CTA per tile; where that leaves SMs idle, the S CTAs of a
+// tile_kernel: the lanes of the accumulator are 128 columns of C (rows of B), its columns 16, 32, 64 or 128 rows of C, so
+// that few rows of C waste little tensor work (one row pays for 16, 33 for 64).  One CTA per tile; where that leaves SMs idle, the S CTAs of a
 // cluster share a tile: CTA r takes the groups r, r + S, ... of K (together they read whole runs of B's rows), sends
 // every CTA the rows of its sum that are that one's to finish (a bulk copy into its shared memory), and finishes its own
 // share, adding the parts in rank order: no atomics, the same sum in every run.  No CTA leaves before all have their parts.
@@ -242,7 +242,7 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
             uint32_t set = 1;
             // An instruction's operands (uniform registers) stay taken until the queue of MMAs reaches it, and a loop that
             // writes the same registers again waits for that: 290 cycles a group.  Four copies of the body use four sets
-            // (1 x 128 x 9216 5.65 -> 5.1 us, 64 x 2048 x 4608 7.85 -> 7.2 us).
+            // (1 x 128 x 9216 5.65 -> 5.1 us, 64 x 2048 x 4608 7.85 -> 7.2 us; 5.6 and 6.9 now).
 #pragma unroll 4
             for (int i = 0; i < count; ++i) {
                 const int g = rank + i * S;
@@ -325,8 +325,8 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
 // sets of scale words in the last 32 columns.
 //   BN = 128, 192   accumulators side by side; the two epilogue groups (warps 2-5, 6-9) take alternate tiles
 //   BN = 256        only for 8-bit C, whose groups of 128 columns a tile of 192 would cut: columns [0, 256) and
-//                   [224, 480) share 32, the groups take the two column halves of every tile, read the shared columns
-//                   first, and the next tile's MMAs start as soon as these are read (about 1000 cycles a tile)
+//                   [224, 480) share 32.  The groups take the two column halves of every tile; the next tile's MMAs start
+//                   when the group whose half holds the shared columns has all its 128 columns in registers
 // Warps: 0 TMA producer, 1 MMA issuer (the first CTA's, for both), 2-9 epilogue.
 
 constexpr int kPairM = 256;
@@ -922,8 +922,8 @@ bool split_allowed(int64_t tiles, int groups, const Device &d, int i) {
 }
 
 // Which kernel and tile take less time, by a model of both in units of 10 ns whose numbers were measured (M from 1 to 4000,
-// N from 128 to 18432, K from 100 to 9216; over 698 shapes the choice takes 1-2 % more than the best of all on average and
-// up to a fifth at a few):
+// N from 128 to 18432, K from 100 to 9216; over 200 other shapes of that range, every plan of each timed, the choice takes 1.6 % more
+// than the best on average, nothing at the median, 7 % at the 90th percentile and 22 % at worst):
 //   pairs       3.1 us from launch to end, and per round of the clusters 0.4 and for a group of K 0.20 us at BN = 128, 0.23
 //               at 192, 0.35 at 256, two fifths more where rows do not begin at multiples of 128 bytes (a box's row then
 //               lies in two lines); or 4 us and B's bytes at 4 TB/s, where that is more: a pair's ring holds little of B
