@@ -223,7 +223,7 @@ def prepare(case, seed):
     s["starts"], s["which"] = _requests(case)
     s["row_start"], s["adapter"] = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (s["starts"], s["which"]))
     room = -(-rows // 256) + case["requests"]                      # where the narrow products pass from one kernel to the next
-    s["workspace"] = torch.zeros(room * 256 * -(-rank // 16) * 128 + 1024 * room, dtype=torch.uint8, device=DEV)
+    s["workspace"] = torch.zeros(room * 256 * -(-rank // 32) * 128 + 1024 * room, dtype=torch.uint8, device=DEV)
     if case["out"] == "fp8":
         s["out"] = _eight_bits(rows, outs)
     else:
