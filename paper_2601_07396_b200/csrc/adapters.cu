@@ -398,12 +398,12 @@ int allow_shared_memory() {
 
 }  // namespace
 
-AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, int out) {
+AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, int parts) {
     AdapterLayout l{};
     l.tiles = (M + tile_rows - 1) / tile_rows;
     l.slots = l.tiles + requests;
     l.narrow_rows = l.slots * tile_rows;
-    l.parts = out == SVDCACHE_BF16 ? 2 : 3;
+    l.parts = parts;
     l.width = l.parts == 3 || rank <= 16 ? 16 : 32;
     l.chunks = (rank + l.width - 1) / l.width;
     l.tile_slots = (size_t)l.narrow_rows * l.chunks * kChunkRow * 2;          // a multiple of 2048

@@ -530,8 +530,8 @@ static int check_adapters(const svdcache_adapters *p, int N, int K) {
 }
 
 /* rows for the highest tiles, tiles and slots for the lowest: room for any plan */
-static size_t adapters_need(int64_t M, int rank, int requests, int out) {
-    const AdapterLayout high = adapter_layout(M, 256, rank, requests, out), low = adapter_layout(M, 16, rank, requests, out);
+static size_t adapters_need(int64_t M, int rank, int requests, int parts) {
+    const AdapterLayout high = adapter_layout(M, 256, rank, requests, parts), low = adapter_layout(M, 16, rank, requests, parts);
     return high.tile_slots + align_up((size_t)low.tiles * 16, kAlign) + align_up((size_t)low.slots * 8, kAlign) + kAlign;
 }
 
@@ -539,7 +539,7 @@ int svdcache_adapters_workspace_bytes(int64_t M, int rank, int requests, size_t 
     if (!bytes) return SVDCACHE_ERR_INVALID_ARG;
     const int rc = check_fp8_shape(M, 1);
     if (rc || rank < 8 || rank > kMaxAdapterRank || rank % 8 || requests < 0 || requests > kMaxRequests) return SVDCACHE_ERR_BAD_SHAPE;
-    *bytes = adapters_need(M, rank, requests, SVDCACHE_F32);             /* the widest */
+    *bytes = adapters_need(M, rank, requests, 3);
     return SVDCACHE_OK;
 }
 
@@ -557,9 +557,9 @@ static int run_gemm_fp8_adapters(const void *A, int64_t lda, const void *SA, con
     if (!row_start || !adapter || !workspace) return SVDCACHE_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(row_start) & 3u) || (reinterpret_cast<uintptr_t>(adapter) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return SVDCACHE_ERR_BAD_ALIGN;
-    if (workspace_bytes < adapters_need(M, adapters->rank, requests, out_dtype)) return SVDCACHE_ERR_WORKSPACE;
-    if (adapter_layout(M, 256, adapters->rank, requests, out_dtype).narrow_rows > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-    const AdapterCall c{*adapters, row_start, adapter, requests, workspace};
+    if (workspace_bytes < adapters_need(M, adapters->rank, requests, 2)) return SVDCACHE_ERR_WORKSPACE;
+    if (adapter_layout(M, 256, adapters->rank, requests, 2).narrow_rows > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    const AdapterCall c{*adapters, row_start, adapter, requests, workspace, workspace_bytes};
     const GemmFp8Plan named{plan && plan[0] != 0, plan ? plan[1] : 0, plan ? plan[2] : 0, 0, 0};
     a.limit = limit_cycles;
     return gemm_fp8_adapters_launch(a, c, plan ? &named : nullptr, (cudaStream_t)stream);

@@ -166,15 +166,15 @@ int gemm_fp8_status_word(int **word);   // the current device's default status w
 // request's, zeros elsewhere, as a sum of bf16 values.  For bf16 output two (off by 2^-16 of the value at most; one would be off by
 // 2^-8, as much as the output's rounding), in chunks of 32 of the rank, or of 16 where that holds it.  For fp32 and 8-bit output
 // three (2^-24), in chunks of 16: a value near a rounding boundary of e4m3 moves by a whole step, and with two parts 7 in 10^5 did,
-// with three 1.4 (9216 x 12288 x 3072, rank 32: 268 and 271 us).  A row of a chunk is kChunkRow values: the first of the two or
-// three, then the seconds, ...
+// with three 1.4 (9216 x 12288 x 3072, rank 32: 268 and 271 us); two where the caller's workspace holds no more.  A row of a chunk is
+// kChunkRow values: the first of the two or three, then the seconds, ...
 constexpr int kChunkRow = 64;
 struct AdapterLayout {
     int64_t tiles, slots, narrow_rows;
     int parts, width, chunks;
     size_t tile_slots, slot_list, total;             // offsets in bytes; narrow lies at 0
 };
-AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, int out);
+AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, int parts);
 
 // the requests of a call as the kernels see them, in tiles of 1 << tile_shift rows
 struct Requests {
@@ -211,6 +211,7 @@ struct AdapterCall {
     const int32_t *row_start, *adapter;
     int requests;
     void *workspace;
+    size_t room;                                     // its bytes
 };
 // for a projection by small tiles that `splits` CTAs share, or by pairs (0); brief: that takes little time
 int adapter_down_launch(const GemmFp8Args &a, const AdapterCall &c, const AdapterLayout &l, int tile_rows, int splits, bool brief, int sms, cudaStream_t s);

@@ -1240,7 +1240,8 @@ int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const G
     if (named && !allowed(a, *named, d)) return SVDCACHE_ERR_INVALID_ARG;
     const GemmFp8Plan plan = named ? *named : choose(a, d);
     const int tile_rows = plan.pairs ? kPairM : plan.size;
-    const AdapterUse use{&c, adapter_layout(a.M, tile_rows, c.pool.rank, c.requests, a.out), tile_rows};
+    AdapterUse use{&c, adapter_layout(a.M, tile_rows, c.pool.rank, c.requests, a.out == SVDCACHE_BF16 ? 2 : 3), tile_rows};
+    if (use.layout.total > c.room) use.layout = adapter_layout(a.M, tile_rows, c.pool.rank, c.requests, 2);
     rc = adapter_down_launch(a, c, use.layout, tile_rows, plan.pairs ? 0 : plan.splits, plan.time < 2500, d.sms, s);
     return rc ? rc : run<true>(a, plan, d, &use, s);
 }
