@@ -528,6 +528,11 @@ SVDCACHE_API int svdcache_selftest_gemm_fp8_adapters(const void *A, int64_t lda,
                                const svdcache_adapters *adapters, const int32_t *row_start, const int32_t *adapter, int requests,
                                void *workspace, size_t workspace_bytes, int32_t *status, const int32_t *plan /* host */,
                                int64_t limit_cycles, void *stream);
+/* How its two kernels, the narrow product's and the projection's, are launched on a device of so many SMs, where the projection is
+ * taken by the given plan and takes little time (brief) or much: CTAs, CTAs of a cluster, columns of tensor memory and bytes
+ * of dynamic shared memory of each, for the one and for the other.  Host only. */
+SVDCACHE_API int svdcache_selftest_adapters_sizes(int64_t M, int N, int K, int rank, int requests, int out_dtype, const int32_t *plan /* host */,
+                               int brief, int sms, int64_t *sizes /* host, out: 8 words */);
 
 #ifdef __cplusplus
 }

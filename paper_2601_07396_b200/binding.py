@@ -84,6 +84,7 @@ SIGNATURES = {
                                          _vp, _vp]),
     "svdcache_selftest_gemm_fp8_adapters": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp, _vp, _ci,
                                                   _vp, _sz, _vp, _vp, _i64, _vp]),
+    "svdcache_selftest_adapters_sizes": (_ci, [_i64, _ci, _ci, _ci, _ci, _ci, _vp, _ci, _ci, _vp]),
     "svdcache_adapter_load": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _ci, ctypes.c_float, _ci, _ci, _ci, _vp]),
     "svdcache_rotary_table": (_ci, [_vp, _i64, _i64, _ci, _ci, _vp, _vp, _vp, _i64, _vp]),
     "svdcache_rotary": (_ci, [_vp, _vp, _i64, _i64, _ci, _ci, _vp, _vp]),
@@ -643,6 +644,13 @@ def svdcache_selftest_gemm_fp8_adapters(A: torch.Tensor, SA: torch.Tensor, B: to
                                                          _ptr(S_out), M, N, K, ctypes.byref(pool), _ptr(row_start), _ptr(adapter), adapter.numel(),
                                                          _ptr(workspace), workspace.numel() * workspace.element_size(), word, words, limit_cycles,
                                                          _stream(stream)), "selftest_gemm_fp8_adapters")
+
+
+def svdcache_selftest_adapters_sizes(M: int, N: int, K: int, rank: int, requests: int, out: int, plan, brief: bool, sms: int = 148):
+    """(CTAs, CTAs of a cluster, columns of tensor memory, bytes of shared memory) of the narrow product's kernel and of the projection's."""
+    out_words = (ctypes.c_int64 * 8)()
+    _check(lib().svdcache_selftest_adapters_sizes(M, N, K, rank, requests, out, (ctypes.c_int32 * 3)(*plan[:3]), int(brief), sms, out_words), "selftest_adapters_sizes")
+    return tuple(out_words[:4]), tuple(out_words[4:])
 
 
 # --------------------------------------------------------------- queries and keys ---

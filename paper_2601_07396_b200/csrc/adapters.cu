@@ -7,6 +7,7 @@
 // cluster where tasks are few; each then adds up a share of the rows from all of them, in rank order.  t leaves as a sum of bf16
 // values, since its other factor is held in bf16 (in 32 bits it would need tf32 MMAs at half of bf16's rate with `up` widened).
 // Warps: 0 finds the task, TMA producer; 1 MMA issuer; 2-5 accumulator -> t.
+#include <algorithm>
 #include <atomic>
 
 #include "fp8.cuh"
@@ -418,49 +419,64 @@ Requests requests_of(const GemmFp8Args &a, const AdapterCall &c, int tile_rows) 
     return q;
 }
 
+namespace {
+int down_columns(int rank) { return rank <= 32 ? 64 : rank <= 96 ? 128 : 256; }
+uint32_t down_stage_bytes(int tile_rows, int rank) { return (uint32_t)(std::min(tile_rows, 128) + (rank + 15) / 16 * 16) * kStageK + 2 * kScalePieceBytes; }
+}  // namespace
+
+size_t adapter_down_beside(int rank) { return shared_for(kBesideProjection, down_columns(rank)); }
+
+KernelSize adapter_down_size(const AdapterLayout &l, int K, int rank, int requests, int tile_rows, int splits, bool brief, int sms) {
+    const int sub = std::min(tile_rows, 128), halves = tile_rows / sub, groups = (int)fp8_groups(K);
+    const uint32_t stage_bytes = down_stage_bytes(tile_rows, rank);
+    KernelSize k{};
+    k.columns = down_columns(rank);
+    // tasks that have work: a tile's, and one more where a request begins in the middle of a tile
+    const int64_t tasks = l.slots * halves, busy = l.tiles * halves + requests - 1;
+    // K is shared by as many CTAs as there are SMs beside a projection of 25 us or less (2048 x 1152 x 4608: 17.9 us with four CTAs a task,
+    // 21.0 with one), and where K is long; beside longer ones fewer CTAs leave more SMs to the projection, which begins on those that
+    // are free (4608 x 9216 x 3072: 104.6 us with four, 102.4 with one; 4608 x 3072 x 12288: 148.7 with one, 144.7 with two, 147.2 with
+    // four).  Beside small tiles half of the SMs (64 x 18432 x 3072, 64 adapters: 40.1 us with two, 37.4 with one).
+    k.cluster = 1;
+    while (k.cluster < 8 && groups >= 4 * k.cluster && (splits > 1 ? 2 * k.cluster <= splits : busy * k.cluster * 2 <= (splits == 1 ? sms / 2 : brief || groups > 48 * k.cluster ? sms : 0)))
+        k.cluster *= 2;
+    k.ctas = tasks * k.cluster;
+    const int longest = (groups + k.cluster - 1) / k.cluster;
+    // an MMA reads 128 rows whatever there are of A: what follows them then stands in rows of the sum that nobody reads
+    const int beyond = (128 - sub) * kStageK;
+    const int most = tile_rows <= 128 ? kBesideProjection : busy * k.cluster > sms ? kTwoOfAnSm : kAlone;
+    k.stages = std::min({(int)((most - 1024 - beyond) / stage_bytes), kMaxStages, longest});
+    const size_t ring = (size_t)k.stages * stage_bytes + (size_t)beyond;
+    const size_t sums = k.cluster == 1 ? 0 : (size_t)sub * ((rank + 31) / 32 * 32 + 4) * 4;
+    k.shared = shared_for(1024 + std::max(ring, sums), k.columns);
+    return k;
+}
+
 int adapter_down_launch(const GemmFp8Args &a, const AdapterCall &c, const AdapterLayout &l, int tile_rows, int splits, bool brief, int sms, cudaStream_t s) {
     int rc = allow_shared_memory();
     if (rc) return rc;
+    const KernelSize k = adapter_down_size(l, a.K, c.pool.rank, c.requests, tile_rows, splits, brief, sms);
     DownParams p{};
     p.q = requests_of(a, c, tile_rows);
     p.tiles = (int)l.tiles; p.slots = (int)l.slots;
     p.sub = tile_rows < 128 ? tile_rows : 128;
     p.halves = tile_rows / p.sub;
     p.rank = c.pool.rank; p.parts = l.parts; p.width = l.width; p.chunks = l.chunks; p.groups = (int)fp8_groups(a.K);
-    p.tmem_cols = p.rank <= 32 ? 64 : p.rank <= 96 ? 128 : 256;
+    p.splits = k.cluster; p.stages = k.stages; p.tmem_cols = k.columns;
     p.x_bytes = (uint32_t)p.sub * kStageK;
-    p.stage_bytes = p.x_bytes + (uint32_t)((p.rank + 15) / 16 * 16) * kStageK + 2 * kScalePieceBytes;
+    p.stage_bytes = down_stage_bytes(tile_rows, p.rank);
     p.pieces = fp8_piece_cols(a.K);
     p.SX = (const uint8_t *)a.SA; p.SD = (const uint8_t *)c.pool.down_scales; p.sd_stride = c.pool.scales_stride;
     p.factor = c.pool.factor;
     char *ws = (char *)c.workspace;
     p.narrow = (__nv_bfloat16 *)ws; p.tile_slots = tile_rows > 128 ? (int4 *)(ws + l.tile_slots) : nullptr; p.slot_list = (int2 *)(ws + l.slot_list);
     p.status = a.status; p.limit = (int)((a.limit > 0 ? a.limit : kWaitCycles) / 1024); p.withhold = a.limit > 0;
-    // tasks that have work: a tile's, and one more where a request begins in the middle of a tile
-    const int64_t tasks = l.slots * p.halves, busy = l.tiles * p.halves + c.requests - 1;
-    // K is shared by as many CTAs as there are SMs beside a projection of 25 us or less (2048 x 1152 x 4608: 17.9 us with four CTAs a task,
-    // 21.0 with one), and where K is long; beside longer ones fewer CTAs leave more SMs to the projection, which begins on those that
-    // are free (4608 x 9216 x 3072: 104.6 us with four, 102.4 with one; 4608 x 3072 x 12288: 148.7 with one, 144.7 with two, 147.2 with
-    // four).  Beside small tiles half of the SMs (64 x 18432 x 3072, 64 adapters: 40.1 us with two, 37.4 with one).
-    p.splits = 1;
-    while (p.splits < 8 && p.groups >= 4 * p.splits && (splits > 1 ? 2 * p.splits <= splits : busy * p.splits * 2 <= (splits == 1 ? sms / 2 : brief || p.groups > 48 * p.splits ? sms : 0)))
-        p.splits *= 2;
-    const int longest = (p.groups + p.splits - 1) / p.splits;
-    // an MMA reads 128 rows whatever there are of A: what follows them then stands in rows of the sum that nobody reads
-    const int beyond = 128 * kStageK - (int)p.x_bytes;
-    const int most = tile_rows <= 128 ? kBesideProjection : busy * p.splits > sms ? kTwoOfAnSm : kAlone;
-    p.stages = (int)((most - 1024 - beyond) / p.stage_bytes);
-    if (p.stages > kMaxStages) p.stages = kMaxStages;
-    if (p.stages > longest) p.stages = longest;
-    size_t smem = (size_t)p.stages * p.stage_bytes + (size_t)beyond;
-    const size_t sums = p.splits == 1 ? 0 : (size_t)p.sub * ((p.rank + 31) / 32 * 32 + 4) * 4;
-    smem = 1024 + (smem > sums ? smem : sums);
-    if (tasks * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    if (k.ctas > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     CUtensorMap tm_x, tm_d;
     rc = byte_map(&tm_x, a.A, 0, a.M, a.K, a.lda, 0, p.sub);
     if (!rc) rc = byte_map(&tm_d, c.pool.down, c.pool.count, c.pool.rank, a.K, c.pool.down_ld, c.pool.down_stride, c.pool.rank);
     if (rc) return rc;
-    return launch_early(down_kernel, dim3((unsigned)(tasks * p.splits)), dim3(kThreads), smem, p.splits, s, tm_x, tm_d, p);
+    return launch_early(down_kernel, dim3((unsigned)k.ctas), dim3(kThreads), k.shared, k.cluster, s, tm_x, tm_d, p);
 }
 
 int adapter_load_launch(const svdcache_adapters &pool, int index, const void *down, int64_t ldd, const void *up, int64_t ldu, int r, float factor,

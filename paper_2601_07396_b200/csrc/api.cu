@@ -1,4 +1,5 @@
 // The extern "C" surface: argument validation, layout queries, dispatch to the kernels.
+#include <algorithm>
 #include <atomic>
 #include <cstdio>
 #include <cmath>
@@ -581,6 +582,21 @@ int svdcache_selftest_gemm_fp8_adapters(const void *A, int64_t lda, const void *
     if (!plan || limit_cycles < 0 || limit_cycles > 200000000LL) return SVDCACHE_ERR_INVALID_ARG;   /* at most ~0.1 s */
     return run_gemm_fp8_adapters(A, lda, SA, B, ldb, SB, bias, act, C, ldc, out_dtype, SC, M, N, K, adapters, row_start, adapter, requests, workspace,
                                  workspace_bytes, status, plan, limit_cycles, stream);
+}
+
+int svdcache_selftest_adapters_sizes(int64_t M, int N, int K, int rank, int requests, int out_dtype, const int32_t *plan, int brief, int sms, int64_t *sizes) {
+    if (!plan || !sizes || (out_dtype != SVDCACHE_F32 && out_dtype != SVDCACHE_BF16 && out_dtype != SVDCACHE_FP8)) return SVDCACHE_ERR_INVALID_ARG;
+    int rc = check_fp8_shape(M, K);
+    if (!rc) rc = check_fp8_shape(1, N);
+    if (rc || M == 0 || rank < 8 || rank > kMaxAdapterRank || rank % 8 || requests < 1 || requests > kMaxRequests || sms < 2) return SVDCACHE_ERR_BAD_SHAPE;
+    const bool pairs = plan[0] != 0;
+    auto in = [](int v, std::initializer_list<int> of) { return std::find(of.begin(), of.end(), v) != of.end(); };
+    if (pairs ? plan[2] != 2 || !in(plan[1], {128, 192, 256}) : !in(plan[1], {16, 32, 64, 128}) || !in(plan[2], {1, 2, 3, 4, 6, 8}) || plan[2] > fp8_groups(K)) return SVDCACHE_ERR_INVALID_ARG;
+    KernelSize size[2];
+    gemm_fp8_adapters_size(M, N, K, rank, requests, out_dtype, {pairs, plan[1], plan[2], 0, 0}, brief != 0, sms, size);
+    for (const KernelSize &k : size)
+        for (int64_t v : {k.ctas, (int64_t)k.cluster, (int64_t)k.columns, (int64_t)k.shared}) *sizes++ = v;
+    return SVDCACHE_OK;
 }
 
 int svdcache_adapter_load(const svdcache_adapters *adapters, int index, const void *down, int64_t ldd, const void *up, int64_t ldu, int r,

@@ -213,7 +213,18 @@ struct AdapterCall {
     void *workspace;
     size_t room;                                     // its bytes
 };
-// for a projection by small tiles that `splits` CTAs share, or by pairs (0); brief: that takes little time
+// how a kernel is launched: CTAs, how many of them a cluster has, dynamic shared memory and columns of tensor memory of each
+struct KernelSize {
+    int64_t ctas;
+    int cluster, columns, stages;
+    size_t shared;
+};
+// The narrow product's, for a projection by small tiles that `splits` CTAs share, or by pairs (0); brief: that takes little time.
+KernelSize adapter_down_size(const AdapterLayout &l, int K, int rank, int requests, int tile_rows, int splits, bool brief, int sms);
+// the most that it asks for beside small tiles
+size_t adapter_down_beside(int rank);
+// both kernels' for a plan, by numbers alone
+void gemm_fp8_adapters_size(int64_t M, int N, int K, int rank, int requests, int out, const GemmFp8Plan &plan, bool brief, int sms, KernelSize (&size)[2]);
 int adapter_down_launch(const GemmFp8Args &a, const AdapterCall &c, const AdapterLayout &l, int tile_rows, int splits, bool brief, int sms, cudaStream_t s);
 Requests requests_of(const GemmFp8Args &a, const AdapterCall &c, int tile_rows);
 int adapter_load_launch(const svdcache_adapters &pool, int index, const void *down, int64_t ldd, const void *up, int64_t ldu, int r, float factor,

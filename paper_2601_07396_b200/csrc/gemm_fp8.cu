@@ -479,7 +479,7 @@ template <int BN> struct Pair {
     static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + 8 * kStoreBytes;
     static constexpr uint32_t kAccStep = kHalves ? 224 : BN;
     static constexpr int kWarpCols = kHalves ? 128 : BN;                          // columns of a tile that a warp finishes
-    static_assert(kStages >= 4 && (BN == 256 || 2 * BN <= (int)kScaleCol), "shared and tensor memory");
+    static_assert(kStages >= 4 && (BN == 256 || 2 * BN <= (int)kScaleCol) && kSmem >= kSharedPerColumn * 512, "shared and tensor memory");
 };
 // Tiles are walked in bands of tile rows, column by column: the clusters at work share a few columns of B's tiles and the
 // band's rows of A.  High bands read B fewer times (4608 x 12288 x 3072 into bf16: 134 us with bands of 8 rows, 130 with
@@ -1039,27 +1039,36 @@ int fill(Adapt<true> *x, const GemmFp8Args &a, const AdapterUse *use, int narrow
     return rc;
 }
 
+uint32_t tile_stage_bytes(int tile_m) { return kBBytes + (uint32_t)tile_m * kStageK + 1024u; }
+// `room`: shared memory of a CTA at most
+KernelSize tile_size(int64_t M, int N, int K, int tile_m, int splits, size_t room) {
+    KernelSize k{};
+    k.ctas = (M + tile_m - 1) / tile_m * ((N + kTileN - 1) / kTileN) * splits;
+    k.cluster = splits;
+    k.columns = tile_m <= 32 ? 64 : 2 * tile_m;                            // the accumulator and 32 columns of scales
+    const size_t sums = (size_t)tile_m * kTileN * 4;                      // pass through the ring,
+    const size_t parts = splits == 1 ? 0 : (size_t)((tile_m + splits - 1) / splits * splits) * kTileN * 4;   // others' arrive behind it
+    static_assert((kSmemLimit - 1024 - 132 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
+    const int longest = (int)((fp8_groups(K) + splits - 1) / splits);
+    k.stages = std::min({(int)((room - 1024 - parts) / tile_stage_bytes(tile_m)), kMaxStages, longest});
+    k.shared = shared_for(1024 + std::max((size_t)k.stages * tile_stage_bytes(tile_m), sums) + parts, k.columns);
+    return k;
+}
+// With adapters, tiles that no CTAs share leave room for a CTA of the narrow product (and for 4 KB of both kernels' own).
+size_t tile_room(int splits, int rank) { return rank == 0 || splits > 1 ? kSmemLimit : std::min((size_t)kBesideNarrow, 224 * 1024 - adapter_down_beside(rank)); }
+
 template <bool ADAPT> int tile_launch(const GemmFp8Args &a, int tile_m, int splits, const AdapterUse *use, cudaStream_t s) {
+    const KernelSize k = tile_size(a.M, a.N, a.K, tile_m, splits, tile_room(splits, ADAPT ? use->call->pool.rank : 0));
     TileParams p{};
     p.M = a.M; p.N = a.N; p.ldc = a.ldc;
     p.SA = (const uint8_t *)a.SA; p.SB = (const uint8_t *)a.SB; p.bias = a.bias; p.C = a.C; p.SC = (uint8_t *)a.SC;
     p.act = a.act; p.out = a.out; p.status = a.status; p.limit = wait_limit(a); p.withhold = a.limit > 0;
     p.groups = (int)fp8_groups(a.K); p.splits = splits; p.n_tiles = (a.N + kTileN - 1) / kTileN; p.tile_m = tile_m;
-    const int64_t tiles = (a.M + tile_m - 1) / tile_m * p.n_tiles;
     p.pieces = fp8_piece_cols(a.K); p.pieces_c = fp8_piece_cols(a.N);
-    if (tiles * p.splits > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
+    if (k.ctas > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     p.a_bytes = (uint32_t)p.tile_m * kStageK;
-    p.stage_bytes = kBBytes + p.a_bytes + 1024u;
-    p.tmem_cols = p.tile_m <= 32 ? 64 : 2 * p.tile_m;                     // the accumulator and 32 columns of scales
-    const size_t sums = (size_t)p.tile_m * kTileN * 4;                    // pass through the ring,
-    const size_t parts = p.splits == 1 ? 0 : (size_t)((p.tile_m + p.splits - 1) / p.splits * p.splits) * kTileN * 4;   // others' arrive behind it
-    static_assert((kSmemLimit - 1024 - 132 * kTileN * 4) / (kBBytes + 128 * kStageK + 1024) >= 2, "a ring has at least two stages");
-    p.stages = (int)(((ADAPT && p.splits == 1 ? kBesideNarrow : kSmemLimit) - 1024 - parts) / p.stage_bytes);
-    if (p.stages > kMaxStages) p.stages = kMaxStages;
-    const int longest = (p.groups + p.splits - 1) / p.splits;
-    if (p.stages > longest) p.stages = longest;
-    size_t smem = (size_t)p.stages * p.stage_bytes;
-    smem = 1024 + std::max(smem, sums) + parts;
+    p.stage_bytes = tile_stage_bytes(p.tile_m);
+    p.tmem_cols = k.columns; p.stages = k.stages;
 
     CUtensorMap tm_a, tm_b;
     int rc = byte_map(&tm_a, a.A, a.M, a.K, a.lda, p.tile_m);
@@ -1068,7 +1077,7 @@ template <bool ADAPT> int tile_launch(const GemmFp8Args &a, int tile_m, int spli
     Adapt<ADAPT> x{};
     rc = fill(&x, a, use, p.tile_m, kTileN);
     if (rc) return rc;
-    return launch_early(tile_kernel<ADAPT>, dim3((unsigned)(tiles * p.splits)), dim3(kTileThreads), smem, p.splits, s, tm_a, tm_b, p, x);
+    return launch_early(tile_kernel<ADAPT>, dim3((unsigned)k.ctas), dim3(kTileThreads), k.shared, k.cluster, s, tm_a, tm_b, p, x);
 }
 
 // a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
@@ -1214,6 +1223,14 @@ int gemm_fp8_status_word(int **word) {
     const int rc = device(&d);
     if (!rc) *word = d.status;
     return rc;
+}
+
+void gemm_fp8_adapters_size(int64_t M, int N, int K, int rank, int requests, int out, const GemmFp8Plan &plan, bool brief, int sms, KernelSize (&size)[2]) {
+    const int tile_rows = plan.pairs ? kPairM : plan.size;
+    size[0] = adapter_down_size(adapter_layout(M, tile_rows, rank, requests, out == SVDCACHE_BF16 ? 2 : 3), K, rank, requests, tile_rows, plan.pairs ? 0 : plan.splits, brief, sms);
+    const int64_t tiles = (M + kPairM - 1) / kPairM * ((N + plan.size - 1) / plan.size);
+    const size_t pair = plan.size == 128 ? Pair<128>::kSmem : plan.size == 192 ? Pair<192>::kSmem : Pair<256>::kSmem;
+    size[1] = plan.pairs ? KernelSize{2 * std::min(tiles, (int64_t)sms / 2), 2, 512, 0, pair} : tile_size(M, N, K, plan.size, plan.splits, tile_room(plan.splits, rank));
 }
 
 int gemm_fp8_plan(const GemmFp8Args &a, GemmFp8Plan *plan) {

@@ -322,6 +322,15 @@ __device__ __forceinline__ uint64_t policy_evict_last() {
 }
 
 // --------------------------------------------------------------------------- tcgen05 ---
+// An SM starts CTAs by their threads and shared memory; where their columns of tensor memory are more than its 512, tcgen05.alloc waits
+// inside one that runs, without a limit.  CTAs of clusters wait for one another while they hold theirs, so such waits could close
+// a circle.  None arises: kernels whose CTAs share SMs ask for 64, 128 or 256 columns (pairs of CTAs for 512) and for this many bytes of
+// shared memory a column at least, so that what fits an SM's 228 KB holds less than 228 KB / 406 = 575.1 columns: no more than 512.  It costs no room:
+// eight CTAs of 64 columns, or two of 256, still fit.
+constexpr size_t kSharedPerColumn = 406;
+static_assert(kSharedPerColumn * (512 + 64) > 228 * 1024, "no CTAs that fit an SM ask for more columns than it has");
+inline size_t shared_for(size_t bytes, int columns) { return bytes > kSharedPerColumn * columns ? bytes : kSharedPerColumn * columns; }
+
 // All of warp `w` executes alloc/dealloc (.sync.aligned).  ncols: power of two in [32, 512].
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols)

@@ -8,7 +8,7 @@ import torch
 
 from paper_2601_07396_b200 import binding as sc
 from tests.fp8_util import check_near, np64, random_fp8
-from tests.test_adapters import NONE, POOL, Pool, P, T, adapted64, cut, ints, random_pool
+from tests.test_adapters import NONE, POOL, Pool, P, T, adapted64, cut, ints, random_pool, run
 from tests.test_fp8_linear import check_padding, half_ulp, junk_fp8
 
 gpu = pytest.mark.gpu
@@ -61,3 +61,99 @@ def test_the_least_workspace_holds_two_values(M, N, K, rank, requests, out):
         close(y, err, C[:, :N], T[out])
     assert sc.gemm_status() == 0
     assert bool((hold[:256] == 0xFF).all()) and bool((hold[-256:] == 0xFF).all())
+
+
+# ---------------------------------------------------------------------- tensor memory and shared memory ---
+
+SM_BYTES, SM_COLUMNS = 228 * 1024, 512
+PLANS = [(0, t, s) for t in (16, 32, 64, 128) for s in (1, 2, 3, 4, 6, 8)] + [(1, n, 2) for n in (128, 192, 256)]
+
+
+def launches(shapes):
+    """((CTAs, of a cluster, columns, bytes) of each kernel) of every rank and plan."""
+    for M, N, K, requests in shapes:
+        for rank in range(8, 129, 8):
+            for plan in PLANS:
+                if not plan[0] and -(-K // 128) < 2 * plan[2] > 2:            # a shared tile gives each CTA two groups of K
+                    continue
+                for out in (sc.F32, sc.BF16):
+                    for brief in (False, True):
+                        yield (M, N, K, requests, rank, plan), sc.svdcache_selftest_adapters_sizes(M, N, K, rank, requests, out, plan, brief)
+
+
+def test_no_set_of_ctas_that_fit_an_sm_asks_for_more_tensor_memory_than_it_has():
+    """An SM starts CTAs by their shared memory; tcgen05.alloc waits without a limit where columns are short, and CTAs of clusters wait for one
+    another while they hold theirs.  So no CTAs of any of these kernels, on any streams, may fit together with more than 512."""
+    least = {}                                            # columns -> the least bytes that a CTA asks for with them
+    clusters = set()
+    shapes = [(M, 512, K, requests) for M in (1, 16, 40, 64, 100, 512, 5000) for K in (1, 128, 129, 300, 520, 1100, 2048, 6300, 40000) for requests in (1, 3, 64, 300)]
+    for which, sizes in launches(shapes):
+        for ctas, cluster, columns, shared in sizes:
+            assert columns in (64, 128, 256, 512) and 0 < shared <= 227 * 1024 and ctas % cluster == 0, which
+            least[columns] = min(least.get(columns, shared), shared)
+        clusters.add(sizes[0][1])
+    assert clusters == {1, 2, 4, 8} and set(least) == {64, 128, 256, 512}
+    # the fewest bytes that hold more columns than an SM has, of any mixture
+    need = {0: 0}
+    for n in range(1, SM_COLUMNS // 64 + 2):
+        need[n] = min(least[c] + need[max(n - c // 64, 0)] for c in least)
+    assert need[SM_COLUMNS // 64 + 1] > SM_BYTES, least
+
+
+def test_ctas_of_the_narrow_product_fit_beside_the_projection_s():
+    """Small tiles that no CTAs share begin beside it; 2 KB are what the system takes, 2 KB the kernels' own."""
+    for which, (narrow, projection) in launches([(1, 512, 3000, 1), (64, 512, 20000, 64), (100, 512, 700, 8)]):
+        if which[-1][0] == 0 and which[-1][2] == 1:
+            assert narrow[3] + projection[3] + 4096 <= SM_BYTES, which
+
+
+MANY = [(64, 512, 2048, 128, 64, "f32"), (512, 256, 2048, 64, 128, "bf16"), (130, 300, 1100, 104, 130, "fp8"), (16, 260, 4100, 128, 16, "bf16"), (600, 520, 1300, 128, 100, "f32")]
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K,rank,requests,out", MANY)
+def test_wide_adapters_of_many_requests(M, N, K, rank, requests, out):
+    run(M, N, K, rank, cut(M, requests, rank), [i * 5 % 9 - 1 for i in range(requests)], 8, out, NONE, True, seed=M)
+
+
+@gpu
+def test_wide_adapters_of_many_requests_on_several_streams():
+    """Each call is bit for bit what it is alone, among others whose CTAs hold as much tensor memory."""
+    jobs = []
+    for i, (M, N, K, rank, requests, out) in enumerate(MANY):
+        a, sa = random_fp8(M, K, i)
+        b, sb = random_fp8(N, K, i + 10, 128)
+        pool = random_pool(8, rank, N, K, i, set(range(8)))
+        jobs.append((a, sa, b, sb, K, pool, ints(cut(M, requests, rank)), ints([j % 9 - 1 for j in range(requests)])))
+    x, plain, side = random_fp8(64, 2048, 5), random_fp8(300, 2048, 6, 128), torch.zeros(64, 304, device=DEV)
+
+    def make():
+        rooms = []
+        for M, N, K, rank, requests, out in MANY:
+            C = sc.new_fp8(M, N) if out == "fp8" else (torch.zeros(M, -(-N // 8) * 8, dtype=T[out], device=DEV), None)
+            rooms.append((C, sc.new_adapters_workspace(M, rank, requests)))
+        return rooms
+
+    def go(i, room, stream=None):
+        (C, s), ws = room
+        a, sa, b, sb, K, pool, start, which = jobs[i]
+        sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, C[:, :MANY[i][1]], pool, start, which, ws, S_out=s, stream=stream)
+
+    want = make()
+    for i, room in enumerate(want):
+        go(i, room)
+    torch.cuda.synchronize()
+    lanes = [(torch.cuda.Stream(), make()) for _ in range(4)]
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for turn in range(10):
+        for n, (stream, rooms) in enumerate(lanes):
+            for i in range(len(jobs)):
+                k = (i + n + turn) % len(jobs)
+                go(k, rooms[k], stream)
+        sc.svdcache_gemm_fp8(*x, *plain, 2048, side[:, :300], stream=other)
+    torch.cuda.synchronize()
+    for _, rooms in lanes:
+        for ((C, _s), _w), ((V, _t), _v) in zip(rooms, want):
+            assert torch.equal(C, V)
+    assert sc.gemm_status() == 0
