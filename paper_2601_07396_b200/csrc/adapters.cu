@@ -80,6 +80,12 @@ __device__ __forceinline__ Task find_task(const DownParams &p, int slot, int lan
 
 // where column n of the rank begins in a row (width 16 or 32)
 __device__ __forceinline__ int place_of(int n, int width) { return (width == 16 ? n >> 4 : n >> 5) * kChunkRow + (n & (width - 1)); }
+// A finite value that would round to bf16's infinity begins with the largest bf16; the rest of an infinity is 0.
+__device__ __forceinline__ float within_bf16(float v) {
+    constexpr float kLargest = 3.38953139e38f;          // (2 - 2^-7) 2^127
+    return fabsf(v) > kLargest && fabsf(v) < __int_as_float(0x7F800000) ? copysignf(kLargest, v) : v;
+}
+__device__ __forceinline__ float rest_of(float v, float part) { return fabsf(v) == __int_as_float(0x7F800000) ? 0.0f : v - part; }
 // eight values -> their parts in bf16, `width` apart, each the rounded rest of those before
 __device__ __forceinline__ void store_parts(__nv_bfloat16 *out, int parts, int width, float (&v)[8]) {
 #pragma unroll
@@ -88,9 +94,9 @@ __device__ __forceinline__ void store_parts(__nv_bfloat16 *out, int parts, int w
         __nv_bfloat162 w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            v[2 * i] -= __low2float(w[i]);
-            v[2 * i + 1] -= __high2float(w[i]);
+            w[i] = __floats2bfloat162_rn(within_bf16(v[2 * i]), within_bf16(v[2 * i + 1]));
+            v[2 * i] = rest_of(v[2 * i], __low2float(w[i]));
+            v[2 * i + 1] = rest_of(v[2 * i + 1], __high2float(w[i]));
         }
         *reinterpret_cast<uint4 *>(out + p * width) = *reinterpret_cast<const uint4 *>(w);
     }

@@ -157,3 +157,32 @@ def test_wide_adapters_of_many_requests_on_several_streams():
         for ((C, _s), _w), ((V, _t), _v) in zip(rooms, want):
             assert torch.equal(C, V)
     assert sc.gemm_status() == 0
+
+
+# ------------------------------------------------------------------------------- sums beyond bf16's range ---
+
+@gpu
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [5, 100, 700])
+def test_narrow_sums_beyond_bf16(M, out):
+    """A row of ones by a `down` of ones is exactly 16, times the factor: infinite, or finite above the largest bf16 (3.3895e38)."""
+    N, K = 40, 16
+    a, sa = sc.new_fp8(M, K)
+    b, sb = sc.new_fp8(N, K)
+    sc.svdcache_quantize_fp8(torch.ones(M, K, device=DEV), a, sa)
+    sc.svdcache_quantize_fp8(torch.zeros(N, K, device=DEV), b, sb, tile_rows=128)
+    sign = torch.where(torch.arange(N, device=DEV) % 2 == 0, 1.0, -1.0)
+    pool = sc.new_adapters(4, 8, N, K)
+    for i, (factor, up) in enumerate([(1e38, 1.0), (-1e38, 1.0), (2.125e37, 2.0 ** -100), (-2.125e37, 2.0 ** -100)]):
+        sc.svdcache_adapter_load(pool, i, torch.ones(1, K, device=DEV), (up * sign)[:, None].contiguous(), factor)
+    C = torch.zeros(M, N, dtype=T[out], device=DEV)
+    starts = [0, 1, 2, M - 2, M - 1, M]
+    sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, C, pool, ints(starts), ints([0, 1, -1, 2, 3]), sc.new_adapters_workspace(M, 8, 5))
+    inf = float("inf") * sign
+    assert torch.equal(C[0].float(), inf) and torch.equal(C[1].float(), -inf) and bool((C[2:M - 2] == 0).all())
+    # t = 16 fl(2.125e37), within 2^-16 (bf16) or 2^-24 of itself, then the product's and the output's rounding
+    want = 16.0 * float(np.float32(2.125e37)) * 2.0 ** -100
+    bound = want * ((2.0 ** -16 + 2.0 ** -8) if out == "bf16" else (2.0 ** -24 + 2.0 ** -22))
+    for row, way in ((M - 2, 1.0), (M - 1, -1.0)):
+        assert np.abs(np64(C[row]) - way * want * np64(sign)).max() <= 1.001 * bound
+    assert sc.gemm_status() == 0
