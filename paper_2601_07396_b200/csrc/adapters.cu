@@ -420,7 +420,7 @@ AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, i
 }
 
 Requests requests_of(const GemmFp8Args &a, const AdapterCall &c, int tile_rows) {
-    Requests q{c.row_start, c.adapter, a.M, c.requests, c.pool.count, 0};
+    Requests q{c.row_start, c.adapter, c.first, a.M, c.requests, c.pool.count, 0};
     while ((1 << q.tile_shift) < tile_rows) ++q.tile_shift;
     return q;
 }

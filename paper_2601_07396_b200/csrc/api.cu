@@ -560,7 +560,7 @@ static int run_gemm_fp8_adapters(const void *A, int64_t lda, const void *SA, con
         return SVDCACHE_ERR_BAD_ALIGN;
     if (workspace_bytes < adapters_need(M, adapters->rank, requests, 2)) return SVDCACHE_ERR_WORKSPACE;
     if (adapter_layout(M, 256, adapters->rank, requests, 2).narrow_rows > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
-    const AdapterCall c{*adapters, row_start, adapter, requests, workspace, workspace_bytes};
+    const AdapterCall c{*adapters, row_start, adapter, requests, workspace, workspace_bytes, 0};
     const GemmFp8Plan named{plan && plan[0] != 0, plan ? plan[1] : 0, plan ? plan[2] : 0, 0, 0};
     a.limit = limit_cycles;
     return gemm_fp8_adapters_launch(a, c, plan ? &named : nullptr, (cudaStream_t)stream);

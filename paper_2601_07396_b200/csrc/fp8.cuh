@@ -166,8 +166,8 @@ int gemm_fp8_status_word(int **word);   // the current device's default status w
 // request's, zeros elsewhere, as a sum of bf16 values.  For bf16 output two (off by 2^-16 of the value at most; one would be off by
 // 2^-8, as much as the output's rounding), in chunks of 32 of the rank, or of 16 where that holds it.  For fp32 and 8-bit output
 // three (2^-24), in chunks of 16: a value near a rounding boundary of e4m3 moves by a whole step, and with two parts 7 in 10^5 did,
-// with three 1.4 (9216 x 12288 x 3072, rank 32: 268 and 271 us); two where the caller's workspace holds no more.  A row of a chunk is
-// kChunkRow values: the first of the two or three, then the seconds, ...
+// with three 1.4 (9216 x 12288 x 3072, rank 32: 268 and 271 us); two for 8-bit output where the caller's workspace holds no more.  A row of a
+// chunk is kChunkRow values: the first of the two or three, then the seconds, ...
 constexpr int kChunkRow = 64;
 struct AdapterLayout {
     int64_t tiles, slots, narrow_rows;
@@ -179,12 +179,12 @@ AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, i
 // the requests of a call as the kernels see them, in tiles of 1 << tile_shift rows
 struct Requests {
     const int32_t *row_start, *adapter;
-    int64_t M;
+    int64_t first, M;                                // the rows that a launch computes: [first, first + M) of the caller's
     int requests, count, tile_shift;
-    // first row of request i (the end for i = requests)
+    // first row of request i (the end for i = requests), counted from the launch's first
     __device__ __forceinline__ int row(int i) const {
-        const int r = row_start[i];
-        return r < 0 ? 0 : (int64_t)r > M ? (int)M : r;
+        const int64_t r = row_start[i] - first;
+        return r < 0 ? 0 : r > M ? (int)M : (int)r;
     }
 };
 // By a whole warp: calls sink(place, first slot, {slot, adapter}), a lane for each, for the slots of a tile that have an adapter, places counted
@@ -212,6 +212,7 @@ struct AdapterCall {
     int requests;
     void *workspace;
     size_t room;                                     // its bytes
+    int64_t first;                                   // row of the caller's that the launch begins with
 };
 // how a kernel is launched: CTAs, how many of them a cluster has, dynamic shared memory and columns of tensor memory of each
 struct KernelSize {

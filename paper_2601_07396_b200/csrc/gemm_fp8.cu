@@ -1164,7 +1164,9 @@ bool split_allowed(int64_t tiles, int groups, const Device &d, int i) {
 //               B's bytes at 5.6 TB/s, where that is more
 // N = 500, K = 100, M = 40: 3.9 us by pairs, 3.8 by small tiles.  N = 500, K = 9000, M = 1 / 40 / 512: 15.0 / 17.7 / 24.3 and
 // 6.2 / 7.4 / 11.2.  N = 18432, K = 3072, M = 1 / 40 / 256: 27.0 / 21.7 / 16.8 and 12.0 / 12.8 / 24.4.
-GemmFp8Plan plan_pair(const GemmFp8Args &a, const Device &d) {
+// (`heights`: the sum of the tiles' rows to choose from.)
+GemmFp8Plan plan_pair(const GemmFp8Args &a, const Device &d, int heights) {
+    if (!(heights & kPairM)) return {};
     const int64_t m_tiles = (a.M + kPairM - 1) / kPairM, groups = fp8_groups(a.K), clusters = d.sms / 2;
     const int64_t fifths = (a.lda | a.ldb) % 128 ? 7 : 5;
     auto plan = [&](int bn, int64_t group) {
@@ -1176,10 +1178,11 @@ GemmFp8Plan plan_pair(const GemmFp8Args &a, const Device &d) {
     return wide.time < narrow.time ? wide : narrow;
 }
 
-GemmFp8Plan plan_tile(const GemmFp8Args &a, const Device &d) {
+GemmFp8Plan plan_tile(const GemmFp8Args &a, const Device &d, int heights) {
     GemmFp8Plan best{};
     const int groups = (int)fp8_groups(a.K), n_tiles = (a.N + kTileN - 1) / kTileN;
     for (int tile_m = least_tile_rows(a.M); tile_m <= most_tile_rows(a.M); tile_m *= 2) {
+        if (!(heights & tile_m)) continue;
         const int64_t tiles = (a.M + tile_m - 1) / tile_m * n_tiles;
         for (int i = 0; i < kSplitKinds; ++i) {
             const int splits = kSplits[i], fit = d.clusters[i];
@@ -1194,9 +1197,10 @@ GemmFp8Plan plan_tile(const GemmFp8Args &a, const Device &d) {
     return best;
 }
 
-GemmFp8Plan choose(const GemmFp8Args &a, const Device &d) {
-    const GemmFp8Plan t = plan_tile(a, d), p = plan_pair(a, d);
-    return t.splits > 0 && t.time < p.time ? t : p;
+// no plan has splits = 0
+GemmFp8Plan choose(const GemmFp8Args &a, const Device &d, int heights = ~0) {
+    const GemmFp8Plan t = plan_tile(a, d, heights), p = plan_pair(a, d, heights);
+    return t.splits > 0 && (p.splits == 0 || t.time < p.time) ? t : p;
 }
 
 bool allowed(const GemmFp8Args &a, const GemmFp8Plan &plan, const Device &d) {
@@ -1248,6 +1252,34 @@ int gemm_fp8_launch(const GemmFp8Args &a, const GemmFp8Plan *plan, cudaStream_t 
     return run<false>(a, plan ? *plan : choose(a, d), d, nullptr, s);
 }
 
+// the heights of tiles for which the workspace holds `parts` values of t, as a sum
+int heights_that_fit(const AdapterCall &c, int64_t M, int parts) {
+    int heights = 0;
+    for (int rows = 16; rows <= kPairM; rows *= 2)
+        if (adapter_layout(M, rows, c.pool.rank, c.requests, parts).total <= c.room) heights += rows;
+    return heights;
+}
+
+// fp32 output shows every rounding of t, so it takes three values in whatever workspace bf16 output does: by lower tiles, which
+// take less room for a request, or by bands of rows one after the other in the same workspace, whichever the model says is faster.  There is always
+// one of the two: two bands of tiles of 128 rows need no more than two values for tiles of 256.
+GemmFp8Plan plan_in_bands(const GemmFp8Args &a, const AdapterCall &c, const Device &d, int64_t *band) {
+    GemmFp8Plan best{};
+    for (int n = 1; n <= 8; ++n) {
+        GemmFp8Args part = a;
+        const int64_t align = n == 2 ? kScaleRows : kPairM;
+        part.M = std::min(a.M, ((a.M + n - 1) / n + align - 1) / align * align);
+        const GemmFp8Plan p = choose(part, d, heights_that_fit(c, part.M, 3));
+        const int64_t bands = (a.M + part.M - 1) / part.M;
+        if (p.splits && (!best.splits || bands * p.time < best.time)) {
+            best = p;
+            best.time = bands * p.time;
+            *band = part.M;
+        }
+    }
+    return best;
+}
+
 // The plan is that of the product alone: the adapters add a stage for every 32 of their rank to each tile, and no plan changes
 // what they add by much.
 int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const GemmFp8Plan *named, cudaStream_t s) {
@@ -1255,12 +1287,28 @@ int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const G
     int rc = device(&d);
     if (rc) return rc;
     if (named && !allowed(a, *named, d)) return SVDCACHE_ERR_INVALID_ARG;
-    const GemmFp8Plan plan = named ? *named : choose(a, d);
+    GemmFp8Plan plan = named ? *named : choose(a, d);
+    int64_t band = a.M;
+    int parts = a.out == SVDCACHE_BF16 ? 2 : 3;
+    if (parts == 3 && !(heights_that_fit(c, a.M, parts) & (plan.pairs ? kPairM : plan.size))) {
+        if (a.out == SVDCACHE_FP8) parts = 2;
+        else if (named) return SVDCACHE_ERR_WORKSPACE;
+        else plan = plan_in_bands(a, c, d, &band);
+    }
     const int tile_rows = plan.pairs ? kPairM : plan.size;
-    AdapterUse use{&c, adapter_layout(a.M, tile_rows, c.pool.rank, c.requests, a.out == SVDCACHE_BF16 ? 2 : 3), tile_rows};
-    if (use.layout.total > c.room) use.layout = adapter_layout(a.M, tile_rows, c.pool.rank, c.requests, 2);
-    rc = adapter_down_launch(a, c, use.layout, tile_rows, plan.pairs ? 0 : plan.splits, plan.time < 2500, d.sms, s);
-    return rc ? rc : run<true>(a, plan, d, &use, s);
+    for (int64_t first = 0; !rc && first < a.M; first += band) {
+        GemmFp8Args part = a;
+        part.M = std::min(band, a.M - first);
+        part.A = (const char *)a.A + first * a.lda;
+        part.SA = (const char *)a.SA + first / kScaleRows * fp8_piece_cols(a.K) * kScalePieceBytes;
+        part.C = (char *)a.C + first * a.ldc * (a.out == SVDCACHE_F32 ? 4 : a.out == SVDCACHE_BF16 ? 2 : 1);
+        AdapterCall call = c;
+        call.first = first;
+        const AdapterUse use{&call, adapter_layout(part.M, tile_rows, c.pool.rank, c.requests, parts), tile_rows};
+        rc = adapter_down_launch(part, call, use.layout, tile_rows, plan.pairs ? 0 : plan.splits, plan.time < 2500, d.sms, s);
+        if (!rc) rc = run<true>(part, plan, d, &use, s);
+    }
+    return rc;
 }
 
 }  // namespace svdc

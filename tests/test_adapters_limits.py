@@ -38,15 +38,17 @@ def test_workspaces_that_are_too_small():
 
 @gpu
 @pytest.mark.parametrize("out", ["f32", "fp8", "bf16"])
-@pytest.mark.parametrize("M,N,K,rank,requests", [(777, 1000, 1160, 24, 7), (40, 260, 700, 128, 3), (300, 700, 640, 72, 2), (4600, 1500, 328, 32, 2), (9, 130, 300, 8, 9)])
+@pytest.mark.parametrize("M,N,K,rank,requests", [(777, 1000, 1160, 24, 7), (40, 260, 700, 128, 3), (300, 700, 640, 72, 2), (4600, 1500, 328, 32, 2), (9, 130, 300, 8, 9),
+                                                    (9200, 260, 330, 32, 3), (9200, 260, 330, 120, 60), (1025, 700, 530, 64, 4), (257, 1000, 2100, 48, 1), (1500, 300, 200, 64, 700)])
 def test_the_least_workspace_holds_two_values(M, N, K, rank, requests, out):
-    """Every type of output in the room that bf16 output needs: then t is within 2^-16, as it is for that."""
+    """Every type of output in the room that bf16 output needs: t is within 2^-16 for 8-bit output, as it is for that, and for fp32 output
+    within 2^-24 all the same."""
     a, sa = random_fp8(M, K, 1)
     b, sb = random_fp8(N, K, 2, 128)
     which = [i % 3 - 1 if i else 0 for i in range(requests)]
     pool = random_pool(2, rank, N, K, 3, set(which))
     starts = cut(M, requests, M)
-    y, err = adapted64(a, sa, b, sb, M, N, K, None, NONE, pool, starts, which, "bf16")
+    y, err = adapted64(a, sa, b, sb, M, N, K, None, NONE, pool, starts, which, "f32" if out == "f32" else "bf16")
     n = least_workspace(M, rank, requests)
     hold = torch.full((n + 512,), 0xFF, dtype=torch.uint8, device=DEV)
     args = (pool, ints(starts), ints(which), hold[256:256 + n])
