@@ -1287,7 +1287,9 @@ int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const G
     int rc = device(&d);
     if (rc) return rc;
     if (named && !allowed(a, *named, d)) return SVDCACHE_ERR_INVALID_ARG;
-    GemmFp8Plan plan = named ? *named : choose(a, d);
+    const GemmFp8Plan chosen = choose(a, d);
+    GemmFp8Plan plan = named ? *named : chosen;
+    const bool brief = chosen.time < 2500;           // by the sizes, so that a named plan has the narrow product that the call has
     int64_t band = a.M;
     int parts = a.out == SVDCACHE_BF16 ? 2 : 3;
     if (parts == 3 && !(heights_that_fit(c, a.M, parts) & (plan.pairs ? kPairM : plan.size))) {
@@ -1305,7 +1307,7 @@ int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const G
         AdapterCall call = c;
         call.first = first;
         const AdapterUse use{&call, adapter_layout(part.M, tile_rows, c.pool.rank, c.requests, parts), tile_rows};
-        rc = adapter_down_launch(part, call, use.layout, tile_rows, plan.pairs ? 0 : plan.splits, plan.time < 2500, d.sms, s);
+        rc = adapter_down_launch(part, call, use.layout, tile_rows, plan.pairs ? 0 : plan.splits, brief, d.sms, s);
         if (!rc) rc = run<true>(part, plan, d, &use, s);
     }
     return rc;

@@ -161,6 +161,22 @@ def test_wide_adapters_of_many_requests_on_several_streams():
     assert sc.gemm_status() == 0
 
 
+# ----------------------------------------------------------------------------------------- named plans ---
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(4096, 8192, 2048), (2048, 4096, 8192), (3000, 2000, 700), (600, 700, 2100), (8, 2304, 1152)])
+def test_the_plan_that_is_reported_gives_what_the_call_gives(M, N, K):
+    """Bit for bit, the narrow product among it: above and below the 25 us from which fewer CTAs share it, with long and shorter K."""
+    a, sa = random_fp8(M, K, 1)
+    b, sb = random_fp8(N, K, 2, 128)
+    pool = random_pool(3, 64, N, K, 3, {0, 1, 2})
+    args = (pool, ints([0, M // 3, M // 2, M]), ints([2, 0, 1]), sc.new_adapters_workspace(M, 64, 3))
+    one, two = (torch.zeros(M, N, device=DEV) for _ in range(2))
+    sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, one, *args)
+    sc.svdcache_selftest_gemm_fp8_adapters(a, sa, b, sb, K, two, *args, sc.svdcache_gemm_fp8_plan(M, N, K, sc.F32, a.stride(0), b.stride(0)))
+    assert torch.equal(one, two) and bool(one.any()) and sc.gemm_status() == 0
+
+
 # ------------------------------------------------------------------------------- sums beyond bf16's range ---
 
 @gpu
