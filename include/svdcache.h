@@ -396,7 +396,9 @@ SVDCACHE_API int svdcache_gemm_fp8_status_query(int32_t *status /* host, out */)
  * Requests are runs of rows: row_start (device, requests + 1 int32, not decreasing) and adapter (device, requests int32; values
  * outside 0 .. count - 1: none).  Rows before the first and behind the last run have no adapter.  Both are read when the
  * call runs, so a captured call serves other requests after they are rewritten.  (Where row_start decreases, rows hold
- * unspecified values; nothing outside the buffers is touched.)  A row's result depends on its own request alone.
+ * unspecified values; nothing outside the buffers is touched.)  Nothing of another request, its rows, its adapter or what these hold, reaches
+ * a row.  The order in which a row's sums are rounded may differ with the sizes of the call and its workspace, the number of its requests and which of
+ * them have an adapter; for the same of these a row is the same bit for bit.
  *
  *   svdcache_adapters_workspace_bytes  room for A down^T between the two kernels of a call, and for which tile has which
  *              adapters; 256-byte aligned, of one call at a time, nothing in it outlives the call.  The size serves any

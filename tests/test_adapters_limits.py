@@ -161,6 +161,33 @@ def test_wide_adapters_of_many_requests_on_several_streams():
     assert sc.gemm_status() == 0
 
 
+# ------------------------------------------------------------------------------------ neighbouring requests ---
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(9, 300, 2100), (60, 300, 700), (64, 18432, 520), (130, 260, 2100), (700, 1300, 600)])
+def test_a_request_among_others(M, N, K):
+    """Rows of one request, by tiles that CTAs share, by tiles of their own and by pairs: with and without adapters beside it, and as one
+    of 1, 3, 5 and more requests, some of which hold NaN, they are what the formula says within the bound of any order of rounding."""
+    a, sa = random_fp8(M, K, 1)
+    b, sb = random_fp8(N, K, 2, 128)
+    pool = random_pool(4, 40, N, K, 3, {0, 1, 2, 3})
+    pool.factor[3] = float("nan")
+    lo, hi = M // 3, M // 3 + max(M // 3, 2)
+    y, err = adapted64(a, sa, b, sb, M, N, K, None, NONE, pool, [lo, hi], [1], "f32")
+    y, err = y[lo:hi], err[lo:hi]
+    each = list(range(lo + 1, hi))                       # a request for each of its rows
+    variants = [([lo, hi], [1]), ([0, lo, hi, M], [-1, 1, -1]), ([0, lo, hi, M], [0, 1, 2]), ([0, lo, hi, M], [3, 1, 3]), ([0, lo // 2, lo, lo, hi, M], [0, 2, 3, 1, 0]),
+                ([0, lo] + each + [hi, M], [3] + [1] * (hi - lo) + [0])]
+    for starts, which in variants:
+        C = torch.zeros(M, N if N % 4 == 0 else -(-N // 4) * 4, device=DEV)[:, :N]
+        twice = torch.zeros_like(C)
+        for out in (C, twice):
+            sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, out, pool, ints(starts), ints(which), sc.new_adapters_workspace(M, 40, len(which)))
+        close(y, err, C[lo:hi], torch.float32)
+        assert torch.equal(C[lo:hi], twice[lo:hi])
+    assert sc.gemm_status() == 0
+
+
 # ----------------------------------------------------------------------------------------- named plans ---
 
 @gpu
