@@ -536,6 +536,13 @@ SVDCACHE_API int svdcache_selftest_gemm_fp8_adapters(const void *A, int64_t lda,
  * of dynamic shared memory of each, for the one and for the other.  Host only. */
 SVDCACHE_API int svdcache_selftest_adapters_sizes(int64_t M, int N, int K, int rank, int requests, int out_dtype, const int32_t *plan /* host */,
                                int brief, int sms, int64_t *sizes /* host, out: 8 words */);
+/* What its kernels find out about requests (all host pointers) of a launch over rows first .. first + M - 1 in tiles of 16, 32, 64, 128 or
+ * 256 rows, by the same code on the host.  S = tiles + requests: tasks (S x 4) the tile, rows and adapter (-1: none) that each slot stands
+ * for; tiles (tiles x 4) where a tile's slots are listed, how many they are, the first one's number and adapter; list (S x 2) those
+ * lists, number and adapter, entries that no tile lists left as they were; tile_list (tiles x (1 + 2 tile_rows)) how many slots a
+ * small tile takes and which. */
+SVDCACHE_API int svdcache_selftest_adapters_slots(const int32_t *row_start, const int32_t *adapter, int requests, int64_t first, int64_t M, int count,
+                               int tile_rows, int32_t *tasks, int32_t *tiles, int32_t *list, int32_t *tile_list);
 
 #ifdef __cplusplus
 }

@@ -85,6 +85,7 @@ SIGNATURES = {
     "svdcache_selftest_gemm_fp8_adapters": (_ci, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _ci, _vp, _i64, _ci, _vp, _i64, _ci, _ci, _vp, _vp, _vp, _ci,
                                                   _vp, _sz, _vp, _vp, _i64, _vp]),
     "svdcache_selftest_adapters_sizes": (_ci, [_i64, _ci, _ci, _ci, _ci, _ci, _vp, _ci, _ci, _vp]),
+    "svdcache_selftest_adapters_slots": (_ci, [_vp, _vp, _ci, _i64, _i64, _ci, _ci, _vp, _vp, _vp, _vp]),
     "svdcache_adapter_load": (_ci, [_vp, _ci, _vp, _i64, _vp, _i64, _ci, ctypes.c_float, _ci, _ci, _ci, _vp]),
     "svdcache_rotary_table": (_ci, [_vp, _i64, _i64, _ci, _ci, _vp, _vp, _vp, _i64, _vp]),
     "svdcache_rotary": (_ci, [_vp, _vp, _i64, _i64, _ci, _ci, _vp, _vp]),
@@ -651,6 +652,19 @@ def svdcache_selftest_adapters_sizes(M: int, N: int, K: int, rank: int, requests
     out_words = (ctypes.c_int64 * 8)()
     _check(lib().svdcache_selftest_adapters_sizes(M, N, K, rank, requests, out, (ctypes.c_int32 * 3)(*plan[:3]), int(brief), sms, out_words), "selftest_adapters_sizes")
     return tuple(out_words[:4]), tuple(out_words[4:])
+
+
+def svdcache_selftest_adapters_slots(row_start: torch.Tensor, adapter: torch.Tensor, M: int, count: int, tile_rows: int, first: int = 0):
+    """(tasks, tiles, list, tile_list) that the kernels find for requests given as int32 tensors on the host; what they leave is -9."""
+    n = adapter.numel()
+    if row_start.dtype != torch.int32 or adapter.dtype != torch.int32 or row_start.is_cuda or adapter.is_cuda or row_start.numel() != n + 1:
+        raise ValueError("row_start and adapter: int32 on the host, one row more than there are adapters")
+    tiles = -(-M // tile_rows)
+    out = [torch.full(shape, -9, dtype=torch.int32) for shape in ((tiles + n, 4), (tiles, 4), (tiles + n, 2), (tiles, 1 + 2 * tile_rows))]
+    row_start, adapter = row_start.contiguous(), adapter.contiguous()
+    _check(lib().svdcache_selftest_adapters_slots(row_start.data_ptr(), adapter.data_ptr(), n, first, M, count, tile_rows, *[t.data_ptr() for t in out]),
+           "selftest_adapters_slots")
+    return tuple(out)
 
 
 # --------------------------------------------------------------- queries and keys ---

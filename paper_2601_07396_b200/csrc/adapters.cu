@@ -43,41 +43,6 @@ struct DownParams {
     int limit, withhold;                              // of every wait, in units of 1024 cycles; `withhold`: nothing is loaded, so that they run out
 };
 
-// by a whole warp: the slots of a tile that have an adapter, listed from the first one's number on (so no two tiles' lists meet)
-__device__ __forceinline__ void write_tile_slots(const DownParams &p, int tile, int lane) {
-    int2 first;
-    const int slots = tile_slots_of(p.q, tile, lane, first, [&](int place, int from, int2 slot) { p.slot_list[from + place] = slot; });
-    if (lane == 0) p.tile_slots[tile] = make_int4(first.x, slots, first.x, first.y);
-}
-
-struct Task { int tile, lo, hi, adapter; };           // rows [lo, hi) of M; adapter < 0: none
-// by a whole warp: the pair that a slot belongs to, the last request whose own first slot is not behind it.  A lane reads all there
-// is to a request at once: this stands before the first load of A.
-__device__ __forceinline__ Task find_task(const DownParams &p, int slot, int lane) {
-    Task t{0, 0, 0, -1};
-    int s = -1, lo = 0, hi = 0, a = -1;
-    for (int i0 = 0; i0 < p.q.requests; i0 += 32) {
-        const int i = i0 + lane;
-        const bool is = i < p.q.requests;
-        const int lo_i = is ? p.q.row(i) : 0, hi_i = is ? p.q.row(i + 1) : 0, a_i = is ? p.q.adapter[i] : -1;
-        const uint32_t begun = __ballot_sync(0xFFFFFFFFu, is && (lo_i >> p.q.tile_shift) + i <= slot);
-        if (!begun) break;
-        const int source = 31 - __clz((int)begun);
-        s = i0 + source;
-        lo = __shfl_sync(0xFFFFFFFFu, lo_i, source);
-        hi = __shfl_sync(0xFFFFFFFFu, hi_i, source);
-        a = __shfl_sync(0xFFFFFFFFu, a_i, source);
-        if (source != 31) break;
-    }
-    t.tile = slot - s;
-    if (s < 0 || t.tile < 0 || t.tile >= p.tiles) return t;
-    const int64_t row0 = (int64_t)t.tile << p.q.tile_shift, end = row0 + (1 << p.q.tile_shift);
-    t.lo = (int)(lo > row0 ? lo : row0);
-    t.hi = (int)(hi < end ? hi : end);
-    if (t.lo < t.hi && a >= 0 && a < p.q.count) t.adapter = a;
-    return t;
-}
-
 // where column n of the rank begins in a row (width 16 or 32)
 __device__ __forceinline__ int place_of(int n, int width) { return (width == 16 ? n >> 4 : n >> 5) * kChunkRow + (n & (width - 1)); }
 // A finite value that would round to bf16's infinity begins with the largest bf16; the rest of an infinity is 0.
@@ -185,14 +150,14 @@ down_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CU
     // holds its tensor memory.
     if (warp == 1) next_may_launch();
     if (warp == 0) {
-        const Task t = find_task(p, slot, lane);
+        const Task t = find_task(Warp{lane}, p.q, p.tiles, slot);
         const int64_t m0 = ((int64_t)t.tile << p.q.tile_shift) + half * p.sub;
         if (lane == 0) task_mem = t;
         if (t.adapter >= 0 && t.lo < m0 + p.sub && t.hi > m0 && elect_one())
             for (int i = 0; i < p.stages && i < loaded; ++i)
                 request_group(tm_x, tm_d, p, base + i * p.stage_bytes, full + 8 * i, rank + i * S, i == 0 || (rank + i * S) % kScaleGroups < S, m0, t.adapter);
     } else if (warp == 2 && p.tile_slots) {
-        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) write_tile_slots(p, (int)t, lane);
+        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) write_tile_slots(Warp{lane}, p.q, (int)t, p.tile_slots, p.slot_list);
     }
     __syncwarp();
     tc_fence_before();

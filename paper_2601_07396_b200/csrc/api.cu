@@ -599,6 +599,27 @@ int svdcache_selftest_adapters_sizes(int64_t M, int N, int K, int rank, int requ
     return SVDCACHE_OK;
 }
 
+int svdcache_selftest_adapters_slots(const int32_t *row_start, const int32_t *adapter, int requests, int64_t first, int64_t M, int count, int tile_rows,
+                                     int32_t *tasks, int32_t *tiles, int32_t *list, int32_t *tile_list) {
+    if (!row_start || !adapter || !tasks || !tiles || !list || !tile_list) return SVDCACHE_ERR_INVALID_ARG;
+    if (requests < 1 || requests > kMaxRequests || first < 0 || M < 1 || M > 0x7FFFFFFFLL || count < 0) return SVDCACHE_ERR_BAD_SHAPE;
+    Requests q{row_start, adapter, first, M, requests, count, 0};
+    while (q.tile_shift < 8 && (1 << q.tile_shift) < tile_rows) ++q.tile_shift;
+    if ((1 << q.tile_shift) != tile_rows || tile_rows < 16) return SVDCACHE_ERR_BAD_SHAPE;
+    const int all = (int)((M + tile_rows - 1) / tile_rows);
+    for (int i = 0; i < all + requests; ++i) {
+        const Task t = find_task(OneThread{}, q, all, i);
+        memcpy(tasks + 4 * (size_t)i, &t, sizeof t);
+    }
+    for (int i = 0; i < all; ++i) {
+        int2 from;
+        write_tile_slots(OneThread{}, q, i, reinterpret_cast<int4 *>(tiles), reinterpret_cast<int2 *>(list));
+        int32_t *own = tile_list + (size_t)i * (2 * tile_rows + 1);
+        own[0] = tile_slots_of(OneThread{}, q, i, tile_rows, from, [&](int place, int, int2 slot) { own[1 + 2 * place] = slot.x; own[2 + 2 * place] = slot.y; });
+    }
+    return SVDCACHE_OK;
+}
+
 int svdcache_adapter_load(const svdcache_adapters *adapters, int index, const void *down, int64_t ldd, const void *up, int64_t ldu, int r,
                           float factor, int N, int K, int dtype, void *stream) {
     NvtxRange range("svdcache_adapter_load");

@@ -19,6 +19,7 @@
 #include <cuda_fp8.h>
 
 #include "internal.cuh"
+#include "slots.cuh"
 
 namespace svdc {
 
@@ -160,9 +161,8 @@ int gemm_fp8_plan(const GemmFp8Args &a, GemmFp8Plan *plan);        // the one th
 int gemm_fp8_launch(const GemmFp8Args &a, const GemmFp8Plan *plan, cudaStream_t s);   // plan null: the model's; else one that it may choose
 int gemm_fp8_status_word(int **word);   // the current device's default status word
 
-// A product with adapters: what lies in the workspace, for tiles of `tile_rows` rows.  A slot is a pair of a tile and a request that
-// have rows in common, tile + request its number: along the rows one of both grows from each pair to the next, so no
-// two pairs share one.  `narrow` holds tile_rows rows for each slot with an adapter: factor * A down^T where the row is the
+// A product with adapters: what lies in the workspace, for tiles of `tile_rows` rows and their slots (slots.cuh).
+// `narrow` holds tile_rows rows for each slot with an adapter: factor * A down^T where the row is the
 // request's, zeros elsewhere, as a sum of bf16 values.  For bf16 output two (off by 2^-16 of the value at most; one would be off by
 // 2^-8, as much as the output's rounding), in chunks of 32 of the rank, or of 16 where that holds it.  For fp32 and 8-bit output
 // three (2^-24), in chunks of 16: a value near a rounding boundary of e4m3 moves by a whole step, and with two parts 7 in 10^5 did,
@@ -176,36 +176,6 @@ struct AdapterLayout {
 };
 AdapterLayout adapter_layout(int64_t M, int tile_rows, int rank, int requests, int parts);
 
-// the requests of a call as the kernels see them, in tiles of 1 << tile_shift rows
-struct Requests {
-    const int32_t *row_start, *adapter;
-    int64_t first, M;                                // the rows that a launch computes: [first, first + M) of the caller's
-    int requests, count, tile_shift;
-    // first row of request i (the end for i = requests), counted from the launch's first
-    __device__ __forceinline__ int row(int i) const {
-        const int64_t r = row_start[i] - first;
-        return r < 0 ? 0 : r > M ? (int)M : (int)r;
-    }
-};
-// By a whole warp: calls sink(place, first slot, {slot, adapter}), a lane for each, for the slots of a tile that have an adapter, places counted
-// from 0; returns how many there are, and in `first` the first one's slot and adapter.
-template <typename F> __device__ __forceinline__ int tile_slots_of(const Requests &q, int tile, int lane, int2 &first, F sink) {
-    const int64_t row0 = (int64_t)tile << q.tile_shift, end = row0 + (1 << q.tile_shift);
-    int slots = 0;
-    first = make_int2(tile, 0);
-    for (int i0 = 0; i0 < q.requests; i0 += 32) {
-        const int i = i0 + lane;
-        const bool is = i < q.requests;
-        const int lo = is ? q.row(i) : 0, hi = is ? q.row(i + 1) : 0, a = is ? q.adapter[i] : -1;
-        const uint32_t with = __ballot_sync(0xFFFFFFFFu, lo < hi && lo < end && hi > row0 && a >= 0 && a < q.count);
-        if (!with) continue;
-        const int source = __ffs((int)with) - 1, a0 = __shfl_sync(0xFFFFFFFFu, a, source);
-        if (slots == 0) first = make_int2(tile + i0 + source, a0);
-        if (with >> lane & 1u) sink(slots + __popc(with & ((1u << lane) - 1u)), first.x, make_int2(tile + i, a));
-        slots += __popc(with);
-    }
-    return slots;
-}
 struct AdapterCall {
     svdcache_adapters pool;
     const int32_t *row_start, *adapter;

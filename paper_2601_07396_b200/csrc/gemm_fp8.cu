@@ -394,10 +394,9 @@ tile_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CU
         // the tile's slots, for the producer and the issuer
         if constexpr (ADAPT) {
             int2 first;
-            const int slots = tile_slots_of(x.q, (int)(m0 / p.tile_m), lane, first, [&](int place, int, int2 slot) {
-                if (place < p.tile_m) slot_mem[place] = slot;            // more than rows only where the requests are not in order
-            });
-            if (lane == 0) slots_mem = min(slots, p.tile_m);
+            // (more than rows only where the requests are not in order)
+            const int slots = tile_slots_of(Warp{lane}, x.q, (int)(m0 / p.tile_m), p.tile_m, first, [&](int place, int, int2 slot) { slot_mem[place] = slot; });
+            if (lane == 0) slots_mem = slots;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(list_bar);

@@ -188,6 +188,95 @@ def test_a_request_among_others(M, N, K):
     assert sc.gemm_status() == 0
 
 
+# ----------------------------------------------------------------------------------------------- slots ---
+
+def random_requests(rng, M, first, tile_rows, ordered):
+    n = int(rng.integers(1, 12) if rng.random() < 0.7 else rng.integers(30, 100))
+    start = np.sort(rng.integers(0, first + M + 40, n + 1)) if ordered else rng.integers(-20, first + M + 40, n + 1)
+    if rng.random() < 0.4:
+        start = first + (start - first) // tile_rows * tile_rows
+    if not ordered and rng.random() < 0.3:
+        start[rng.integers(0, n + 1)] = rng.choice([-(1 << 31), (1 << 31) - 1])
+    return start, rng.integers(-1, 5, n)
+
+
+@pytest.mark.parametrize("tile_rows", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("ordered", [True, False])
+def test_what_the_kernels_find_out_about_requests(tile_rows, ordered):
+    """Their own code: each pair of a tile and a request with rows in common has one slot, which knows it, and no two tiles' lists meet.
+    Whatever the rows say, nothing outside the tables is written (the guards around them) and no index leads out of them."""
+    rng = np.random.default_rng(tile_rows)
+    count = 3
+    L = sc.lib()
+    for _ in range(150):
+        M, first = int(rng.integers(1, 900)), int(rng.integers(0, 3)) * 256
+        start, which = random_requests(rng, M, first, tile_rows, ordered)
+        n, tiles = len(which), -(-M // tile_rows)
+        s32, w32 = torch.tensor(start, dtype=torch.int32), torch.tensor(which, dtype=torch.int32)
+        room = [np.full((k + 2, 2 + m), -9, dtype=np.int32).reshape(-1) for k, m in ((tiles + n, 4), (tiles, 4), (tiles + n, 2), (tiles, 1 + 2 * tile_rows))]
+        sizes = [(tiles + n) * 4, tiles * 4, (tiles + n) * 2, tiles * (1 + 2 * tile_rows)]
+        assert L.svdcache_selftest_adapters_slots(s32.data_ptr(), w32.data_ptr(), n, first, M, count, tile_rows, *[r.ctypes.data + 16 for r in room]) == 0
+        for r, size in zip(room, sizes):
+            assert (r[:4] == -9).all() and (r[4 + size:] == -9).all()
+        tasks, entries, listed, own = (r[4:4 + size].reshape(-1, k) for r, size, k in zip(room, sizes, (4, 4, 2, 1 + 2 * tile_rows)))
+        for got, want in zip(sc.svdcache_selftest_adapters_slots(s32, w32, M, count, tile_rows, first), (tasks, entries, listed, own)):
+            assert (got.numpy() == want).all()
+        rows = np.clip(start - first, 0, M)
+        taken = set()
+        assert ((tasks[:, 3] < 0) | ((tasks[:, 0] >= 0) & (tasks[:, 0] < tiles) & (tasks[:, 1] >= 0) & (tasks[:, 1] < tasks[:, 2]) & (tasks[:, 2] <= M) & (tasks[:, 3] < count))).all()
+        for tile in range(tiles):
+            place, many, number, adapter = entries[tile]
+            got = listed[place:place + many]
+            assert 0 <= place and 0 <= many and place + many <= tiles + n
+            assert 0 <= own[tile, 0] <= tile_rows
+            mine = own[tile, 1:1 + 2 * own[tile, 0]].reshape(-1, 2)
+            for part in (got, mine):
+                assert ((part[:, 0] >= 0) & (part[:, 0] < tiles + n) & (part[:, 1] >= 0) & (part[:, 1] < count)).all()
+            assert many == 0 or (0 <= number < tiles + n and 0 <= adapter < count)
+            if ordered:
+                want = [(tile, max(a, tile * tile_rows), min(b, (tile + 1) * tile_rows), w) for a, b, w in zip(rows, rows[1:], which)
+                        if min(b, (tile + 1) * tile_rows) > max(a, tile * tile_rows) and 0 <= w < count]
+                assert [tuple(tasks[j]) for j, _ in got] == want and (got == mine).all() and (many == 0 or tuple(got[0]) == (number, adapter))
+                places = set(range(place, place + many))
+                assert not taken & places
+                taken |= places
+
+
+ANY_ROWS = [[40, 10, 70, 20, 5], [-5, 1 << 30, -(1 << 31), 3, (1 << 31) - 1], [30, 30, 0, 64, 0], [63, 62, 61, 60, 59], [1000, 900, 800, 0, 2000]]
+
+
+@gpu
+@pytest.mark.parametrize("M,N,plan,out", [(64, 260, (0, 64, 1), "f32"), (64, 260, (0, 64, 4), "f32"), (300, 130, (0, 128, 2), "bf16"), (600, 700, (1, 128, 2), "bf16"), (600, 700, (1, 256, 2), "fp8")])
+def test_rows_in_no_order(M, N, plan, out):
+    """Rows that decrease or lie outside: the call ends, with nothing outside its buffers touched, and the next one is in order.  (More
+    requests than a small tile has rows among them.)"""
+    K, rank = 1200, 24
+    a, sa = random_fp8(M, K, 1)
+    b, sb = random_fp8(N, K, 2, 128)
+    pool = random_pool(3, rank, N, K, 3, {0, 1, 2})
+    rng = np.random.default_rng(M)
+    cases = [(s, [0, 1, 2, 0]) for s in ANY_ROWS] + [([int(x) for x in rng.integers(-20, M + 20, 201)], [int(x) for x in rng.integers(-1, 4, 200)]) for _ in range(3)]
+    for i, (starts, which) in enumerate(cases + [([0, 20, M - 5, M], [2, -1, 1])]):
+        n = sc.svdcache_adapters_workspace_bytes(M, rank, len(which))
+        hold = torch.full((n + 512,), 0xFF, dtype=torch.uint8, device=DEV)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        args = (pool, ints(starts), ints(which), hold[256:256 + n], plan)
+        if out == "fp8":
+            q, s = junk_fp8(M, N)
+            sc.svdcache_selftest_gemm_fp8_adapters(a, sa, b, sb, K, q[:, :N], *args, S_out=s, status=status)
+            check_padding(q, s, M, N)
+        else:
+            C = torch.full((M + 2, -(-N // 8) * 8 + 8), 7.0, dtype=T[out], device=DEV)
+            sc.svdcache_selftest_gemm_fp8_adapters(a, sa, b, sb, K, C[1:-1, :N], *args, status=status)
+            assert bool((C[1:-1, N:] == 7.0).all()) and bool((C[0] == 7.0).all()) and bool((C[-1] == 7.0).all())
+        assert int(status) == 0 and bool((hold[:256] == 0xFF).all()) and bool((hold[-256:] == 0xFF).all())
+    y, err = adapted64(a, sa, b, sb, M, N, K, None, NONE, pool, starts, which, out)
+    if out == "fp8":
+        check_near(q, s, y, err)
+    else:
+        close(y, err, C[1:-1, :N], T[out])
+
+
 # ----------------------------------------------------------------------------------------- named plans ---
 
 @gpu
