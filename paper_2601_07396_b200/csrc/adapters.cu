@@ -407,9 +407,10 @@ KernelSize adapter_down_size(const AdapterLayout &l, int K, int rank, int reques
     // K is shared by as many CTAs as there are SMs beside a projection of 25 us or less (2048 x 1152 x 4608: 17.9 us with four CTAs a task,
     // 21.0 with one), and where K is long; beside longer ones fewer CTAs leave more SMs to the projection, which begins on those that
     // are free (4608 x 9216 x 3072: 104.6 us with four, 102.4 with one; 4608 x 3072 x 12288: 148.7 with one, 144.7 with two, 147.2 with
-    // four).  Beside small tiles half of the SMs (64 x 18432 x 3072, 64 adapters: 40.1 us with two, 37.4 with one).
+    // four).  Beside small tiles half of the SMs (64 x 18432 x 3072, 64 adapters: 40.1 us with two, 37.4 with one); beside shared ones no more
+    // CTAs than share the projection's tiles, and than there are SMs (64 x 512 x 2048, 64 requests of rank 128: 44.7 us with eight, 40.1 with two).
     k.cluster = 1;
-    while (k.cluster < 8 && groups >= 4 * k.cluster && (splits > 1 ? 2 * k.cluster <= splits : busy * k.cluster * 2 <= (splits == 1 ? sms / 2 : brief || groups > 48 * k.cluster ? sms : 0)))
+    while (k.cluster < 8 && groups >= 4 * k.cluster && (splits > 1 ? 2 * k.cluster <= splits && busy * k.cluster * 2 <= sms : busy * k.cluster * 2 <= (splits == 1 ? sms / 2 : brief || groups > 48 * k.cluster ? sms : 0)))
         k.cluster *= 2;
     k.ctas = tasks * k.cluster;
     const int longest = (groups + k.cluster - 1) / k.cluster;

@@ -102,6 +102,13 @@ def test_no_set_of_ctas_that_fit_an_sm_asks_for_more_tensor_memory_than_it_has()
     assert need[SM_COLUMNS // 64 + 1] > SM_BYTES, least
 
 
+def test_shared_tasks_of_the_narrow_product_are_no_more_than_sms():
+    for (M, N, K, requests, rank, plan), (narrow, _) in launches([(64, 512, 2048, 64), (512, 256, 2048, 128), (40, 512, 9000, 1), (5000, 512, 40000, 3)]):
+        rows = 256 if plan[0] else plan[1]
+        tasks = -(-M // rows) * (2 if plan[0] else 1) + requests - 1
+        assert narrow[1] == 1 or tasks * narrow[1] <= 148, (M, N, K, requests, rank, plan)
+
+
 def test_ctas_of_the_narrow_product_fit_beside_the_projection_s():
     """Small tiles that no CTAs share begin beside it; 2 KB are what the system takes, 2 KB the kernels' own."""
     for which, (narrow, projection) in launches([(1, 512, 3000, 1), (64, 512, 20000, 64), (100, 512, 700, 8)]):
