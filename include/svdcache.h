@@ -408,7 +408,8 @@ SVDCACHE_API int svdcache_gemm_fp8_status_query(int32_t *status /* host, out */)
  *              into the second product as a sum of two bf16 values for bf16 output (off by 2^-16
  *              of itself at most), of three for the others (2^-24).  Where the workspace is
  *              smaller than svdcache_adapters_workspace_bytes and does not hold three, 8-bit output takes two, and fp32 output three by lower
- *              tiles or several launches, which may take longer.  0 requests or count 0: svdcache_gemm_fp8.
+ *              tiles or several launches, which may take longer.  Kernel and
+ *              tiles are those of the product alone (svdcache_gemm_fp8_plan), which with many requests are not always the fastest.  0 requests or count 0: svdcache_gemm_fp8.
  *   svdcache_adapter_load  puts an adapter into place `index` of a pool: down (r x K) into 8 bits with a scale per 1 x 128 group, up
  *              (N x r) into bf16, both F32 or BF16 (dtype) with 16-byte aligned rows (up: any pitch), r <= rank, factor.  Where a value
  *              of up does not become a finite bf16 it is held as 0 and the adapter's factor as NaN: all rows that use it

@@ -195,7 +195,8 @@ down_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CU
         if (elect_one()) {
             int s = 0;
             uint32_t ph = 0, set = 1;
-            // scale words: four columns for A, then four for down; two sets that alternate
+            // scale words: four columns for A, which are read up to two columns further where x_word is 2, and from the eighth on four for down; two
+            // sets that alternate
             const uint32_t sf = tmem + (uint32_t)p.tmem_cols - 32u;
             const uint32_t x_word = (uint32_t)(m0 % kScaleRows) / 32u;   // 0 or 2: a task of 64 rows may begin in the middle of a piece
             const int n = (p.rank + 15) / 16 * 16;                       // columns beyond the rank come from rows that were not loaded
