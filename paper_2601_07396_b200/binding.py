@@ -588,7 +588,7 @@ def new_adapters(count: int, rank: int, N: int, K: int, device="cuda") -> Adapte
 
 def svdcache_adapter_load(adapters: Adapters, index: int, down: torch.Tensor, up: torch.Tensor, factor: float = 1.0, stream=None) -> None:
     """Puts an adapter, down [r, K] and up [N, r] both fp32 or both bf16, into place `index` of a pool of rank r or more: down in 8 bits with
-    a scale per 1 x 128 group, up in bf16.  If a value of up is not finite there, the factor becomes NaN, and with it every row
+    a scale per 1 x 128 group (e4m3: x down^T is off by about 2.6 % of its norm), up in bf16.  If a value of up is not finite there, the factor becomes NaN, and with it every row
     that uses the adapter."""
     rc = (_calls or calls()).adapter_load(*adapters, index, down, up, factor, None if stream is None else stream.cuda_stream)
     if rc:

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2601_07396_b200 import binding as sc
-from tests.fp8_util import check_near, np64, random_fp8
+from tests.fp8_util import check_near, dequantise, np64, random_fp8
 from tests.test_adapters import NONE, POOL, Pool, P, T, adapted64, cut, ints, random_pool, run
 from tests.test_fp8_linear import check_padding, half_ulp, junk_fp8
 
@@ -326,4 +326,27 @@ def test_narrow_sums_beyond_bf16(M, out):
     bound = want * ((2.0 ** -16 + 2.0 ** -8) if out == "bf16" else (2.0 ** -24 + 2.0 ** -22))
     for row, way in ((M - 2, 1.0), (M - 1, -1.0)):
         assert np.abs(np64(C[row]) - way * want * np64(sign)).max() <= 1.001 * bound
+    assert sc.gemm_status() == 0
+
+
+# ------------------------------------------------------------------------------- an adapter as its user has it ---
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K", [1152, 12288])
+def test_the_adapter_s_term_against_the_adapter_before_it_is_rounded(K, dtype):
+    """A value of `down` in e4m3 is off by at most 2^-4 of the power of two below it, evenly spread: 2^-4 / sqrt(3) of itself in the mean square, and so
+    is a sum of many; 4096 outputs of 16 sums are within a tenth of that."""
+    M, N, r = 64, 64, 16
+    g = torch.Generator().manual_seed(K)
+    x, down, up = torch.randn(M, K, generator=g), torch.randn(r, K, generator=g) / K ** 0.5, torch.randn(N, r, generator=g).bfloat16()
+    (a, sa), (b, sb) = sc.new_fp8(M, K), sc.new_fp8(N, K)
+    sc.svdcache_quantize_fp8(x.to(DEV), a, sa)
+    sc.svdcache_quantize_fp8(torch.zeros(N, K, device=DEV), b, sb, tile_rows=128)
+    pool, C = sc.new_adapters(1, r, N, K), torch.zeros(M, N, device=DEV)
+    down = down.to(dtype).to(DEV)
+    sc.svdcache_adapter_load(pool, 0, down, up.to(dtype).to(DEV), 2.0)
+    sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, C, pool, ints([0, M]), ints([0]), sc.new_adapters_workspace(M, r, 1))
+    want = 2.0 * (dequantise(a, sa, M, K) @ np64(down).T) @ np64(up).T
+    assert np.linalg.norm(np64(C) - want) <= 1.1 * 2.0 ** -4 / 3 ** 0.5 * np.linalg.norm(want)
     assert sc.gemm_status() == 0
