@@ -1281,8 +1281,8 @@ GemmFp8Plan plan_in_bands(const GemmFp8Args &a, const AdapterCall &c, const Devi
 
 // The plan is that of the product alone, which knows neither rank nor requests.  The adapters add a stage to a tile for each of its requests
 // and every 32 of the rank (16 where that holds it, or with three parts): a pair's tile of 256 rows runs all of them one after the other, while
-// small tiles have fewer requests each and may share their stages.  Over 100 random shapes with 1 to 256 requests the choice takes 5.5 % more than the best
-// plan on average, 0.3 % at the median, 23 % at the 90th percentile and 54 % at worst (214 x 296 x 576, 72 requests: 23.4 us by pairs, 15.2 by tiles
+// small tiles have fewer requests each and may share their stages.  Over 100 random shapes with 1 to 256 requests the choice takes 5.7 % more than the best
+// plan on average, 0.6 % at the median, 22 % at the 90th percentile and 54 % at worst (214 x 296 x 576, 72 requests: 22.8 us by pairs, 14.8 by tiles
 // of 64 rows).
 int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const GemmFp8Plan *named, cudaStream_t s) {
     Device d;
