@@ -528,7 +528,8 @@ SVDCACHE_API int svdcache_selftest_gemm_fp8(const void *A, int64_t lda, const vo
                                const void *SB, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
                                void *SC, int64_t M, int N, int K, int32_t *status, const int32_t *plan /* host */,
                                int64_t limit_cycles, void *stream);
-/* the same for svdcache_gemm_fp8_adapters (which takes its projection as svdcache_gemm_fp8_plan says), with a request and an adapter at least */
+/* the same for svdcache_gemm_fp8_adapters (which takes its projection as svdcache_gemm_fp8_plan says), with a request and an adapter at least, and room for
+ * three values of t for fp32 output */
 SVDCACHE_API int svdcache_selftest_gemm_fp8_adapters(const void *A, int64_t lda, const void *SA, const void *B, int64_t ldb, const void *SB,
                                const float *bias, int act, void *C, int64_t ldc, int out_dtype, void *SC, int64_t M, int N, int K,
                                const svdcache_adapters *adapters, const int32_t *row_start, const int32_t *adapter, int requests,

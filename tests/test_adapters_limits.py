@@ -65,6 +65,44 @@ def test_the_least_workspace_holds_two_values(M, N, K, rank, requests, out):
     assert bool((hold[:256] == 0xFF).all()) and bool((hold[-256:] == 0xFF).all())
 
 
+@gpu
+def test_bands_of_rows_in_a_graph():
+    """fp32 output in the least workspace by several launches, captured once and replayed for other requests, twice on two streams at once."""
+    M, N, K, rank, requests = 9200, 264, 520, 32, 2
+    a, sa = random_fp8(M, K, 1)
+    b, sb = random_fp8(N, K, 2, 128)
+    pool = random_pool(3, rank, N, K, 3, {0, 1, 2})
+    plans = [([0, 4000, M], [0, 1]), ([0, 3071, 3073], [2, 0]), ([9000, 9100, 9199], [1, 2]), ([4607, 4608, 4609], [0, 2])]
+    lanes = []
+    for _ in range(2):
+        C, ws = torch.zeros(M, N, device=DEV), torch.full((least_workspace(M, rank, requests),), 0xFF, dtype=torch.uint8, device=DEV)
+        start, which, stream = ints(plans[0][0]), ints(plans[0][1]), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        before = sc.svdcache_kernel_launches()
+        sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, C, pool, start, which, ws, stream=stream)
+        assert sc.svdcache_kernel_launches() - before >= 4          # two of each band
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            sc.svdcache_gemm_fp8_adapters(a, sa, b, sb, K, C, pool, start, which, ws)
+        lanes.append((C, start, which, stream, graph))
+    for i in range(len(plans)):
+        now = [plans[(i + j) % len(plans)] for j in range(2)]
+        for (C, start, which, stream, graph), (s, w) in zip(lanes, now):
+            C.zero_()
+            start.copy_(ints(s))
+            which.copy_(ints(w))
+        torch.cuda.synchronize()
+        for C, start, which, stream, graph in lanes:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (C, *_), (s, w) in zip(lanes, now):
+            y, err = adapted64(a, sa, b, sb, M, N, K, None, NONE, pool, s, w, "f32")
+            close(y, err, C, torch.float32)
+    assert sc.gemm_status() == 0
+
+
 # ---------------------------------------------------------------------- tensor memory and shared memory ---
 
 SM_BYTES, SM_COLUMNS = 228 * 1024, 512
