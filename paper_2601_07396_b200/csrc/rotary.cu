@@ -15,7 +15,7 @@ namespace {
 // ---------------------------------------------------------------------------------------------- table ---
 
 constexpr int kTableThreads = 256, kTableSteps = 4;      // of a CTA; tokens that a thread has under way
-constexpr int kTableCtas = 592;                          // at most: all that are at work at once
+constexpr int kTableCtas = 592;                          // at most: all that are at work at once (of int64 positions 444 are)
 
 struct TableArgs {
     double2 turns[SVDCACHE_ROTARY_MAX_DIM / 4];          // of two neighbouring pairs, per unit of position
@@ -47,8 +47,9 @@ __device__ __forceinline__ float2 cos_sin_of_turns(double t) {
 
 // A thread keeps two neighbouring pairs, whose speeds it reads once (lanes that read different words of the parameters wait
 // for one another: reading them for four tokens each made 48 us of 118800 tokens), and walks over the tokens, the next ones'
-// positions on their way meanwhile (118800 tokens of 64 pairs: 20 -> 16 us, 3.9 TB/s; 9.6 would be the bytes, and the 2.6
-// 64-bit and 40 32-bit instructions of a pair take 8.6 of issue).
+// positions on their way meanwhile (118800 tokens of 64 pairs: 20 -> 16 us, 3.9 TB/s, int64 18).  The bytes
+// would take 9.6 and the 2.6 64-bit and 40 32-bit instructions of a pair 8.6 of issue, beside one another; the rest is half of an SM's threads, or
+// fewer (64 registers, 76 for int64), and 592 CTAs that walk 6.3 rounds as seven.
 template <typename P> __global__ void __launch_bounds__(kTableThreads) table_kernel(const __grid_constant__ TableArgs a) {
     const int row = (int)threadIdx.x / a.columns, column = (int)threadIdx.x - row * a.columns;
     if (row >= a.at_once) return;

@@ -326,7 +326,8 @@ __device__ __forceinline__ uint64_t policy_evict_last() {
 // inside one that runs, without a limit.  CTAs of clusters wait for one another while they hold theirs, so such waits could close
 // a circle.  None arises: kernels whose CTAs share SMs ask for 64, 128 or 256 columns (pairs of CTAs for 512) and for this many bytes of
 // shared memory a column at least, so that what fits an SM's 228 KB holds less than 228 KB / 406 = 575.1 columns: no more than 512.  It costs no room:
-// eight CTAs of 64 columns, or two of 256, still fit.
+// eight CTAs of 64 columns, or two of 256, still fit.  (The step and Gram kernels take all columns and 193 KB or more: beside such a CTA, which waits for
+// no other, one of these fits.)
 constexpr size_t kSharedPerColumn = 406;
 static_assert(kSharedPerColumn * (512 + 64) > 228 * 1024, "no CTAs that fit an SM ask for more columns than it has");
 inline size_t shared_for(size_t bytes, int columns) { return bytes > kSharedPerColumn * columns ? bytes : kSharedPerColumn * columns; }
