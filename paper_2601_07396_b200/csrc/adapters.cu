@@ -11,6 +11,7 @@
 #include <atomic>
 
 #include "fp8.cuh"
+#include "maps.cuh"
 #include "umma.cuh"
 
 namespace svdc {
@@ -324,37 +325,6 @@ template <typename T> __global__ void up_kernel(const LoadArgs a) {
 
 // ------------------------------------------------------------------------- host side ---
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = [] {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(ptr);
-        return (EncodeTiledFn) nullptr;
-    }();
-    return fn;
-}
-
-// bytes [count x rows x cols] in boxes of 1 x box_rows x 128; bytes beyond a matrix read as zero
-int byte_map(CUtensorMap *m, const void *base, int64_t count, int64_t rows, int cols, int64_t ld, int64_t stride, int box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return SVDCACHE_ERR_CUDA;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
-    const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)stride};
-    const cuuint32_t box[3] = {(cuuint32_t)kStageK, (cuuint32_t)box_rows, 1};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, count > 0 ? 3 : 2, const_cast<void *>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, ld % 256 == 0 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
-}
-
 // leave to use an SM's shared memory, asked for once per device
 int allow_shared_memory() {
     static std::atomic<bool> done[64];
@@ -446,8 +416,8 @@ int adapter_down_launch(const GemmFp8Args &a, const AdapterCall &c, const Adapte
     p.status = a.status; p.limit = (int)((a.limit > 0 ? a.limit : kWaitCycles) / 1024); p.withhold = a.limit > 0;
     if (k.ctas > 0x7FFFFFFFLL) return SVDCACHE_ERR_BAD_SHAPE;
     CUtensorMap tm_x, tm_d;
-    rc = byte_map(&tm_x, a.A, 0, a.M, a.K, a.lda, 0, p.sub);
-    if (!rc) rc = byte_map(&tm_d, c.pool.down, c.pool.count, c.pool.rank, a.K, c.pool.down_ld, c.pool.down_stride, c.pool.rank);
+    rc = byte_map(&tm_x, a.A, a.M, a.K, a.lda, p.sub);
+    if (!rc) rc = byte_map(&tm_d, c.pool.down, c.pool.rank, a.K, c.pool.down_ld, c.pool.rank, c.pool.count, c.pool.down_stride);
     if (rc) return rc;
     return launch_early(down_kernel, dim3((unsigned)k.ctas), dim3(kThreads), k.shared, k.cluster, s, tm_x, tm_d, p);
 }

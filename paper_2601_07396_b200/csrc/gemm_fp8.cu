@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "fp8.cuh"
+#include "maps.cuh"
 #include "umma.cuh"
 
 namespace svdc {
@@ -902,41 +903,6 @@ done:
 
 // ------------------------------------------------------------------------- host side ---
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = [] {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(ptr);
-        return (EncodeTiledFn) nullptr;
-    }();
-    return fn;
-}
-
-// bytes [rows x cols], rows `ld` bytes apart, boxes of 128 bytes x box_rows with the 128-byte swizzle; bytes
-// beyond the matrix read as zero, which is e4m3's zero.  Where rows begin at multiples of 256 bytes, L2 fetches so many
-// at a time, two groups of K that are read one after the other (1 x 18432 x 9216 31.7 -> 29.5 us); elsewhere half of such
-// a fetch may belong to another row (256 x 6912 x 9000 27.1 -> 29.3 us, 40 x 18432 x 400 4.8 -> 5.2).
-int byte_map(CUtensorMap *m, const void *base, int64_t rows, int cols, int64_t ld, int box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return SVDCACHE_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {(cuuint32_t)kStageK, (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          ld % 256 == 0 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SVDCACHE_OK : SVDCACHE_ERR_CUDA;
-}
-
 // CTAs per tile of tile_kernel.  (3 and 6 for numbers of tiles that leave SMs to 2 and 4: 256 x 1152 x 9000 16.6 -> 13.2 us.)
 constexpr int kSplits[] = {1, 2, 3, 4, 6, 8}, kSplitKinds = 6;
 
@@ -1005,7 +971,7 @@ int wait_limit(const GemmFp8Args &a) { return (int)((a.limit > 0 ? a.limit : kWa
 // a bf16 matrix, or `count` of them `stride` elements apart, in boxes of box_rows x box_cols as wide as their swizzle; elements
 // beyond a matrix read as zero
 int bf16_map(CUtensorMap *m, const void *base, int64_t count, int64_t rows, int cols, int64_t ld, int64_t stride, int box_rows, int box_cols) {
-    EncodeTiledFn fn = encode_fn();
+    EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return SVDCACHE_ERR_CUDA;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2};
@@ -1082,7 +1048,7 @@ template <bool ADAPT> int tile_launch(const GemmFp8Args &a, int tile_m, int spli
 // a scale buffer as rows of 128-row strips, each `pieces` pieces of 128 words; boxes of one piece.  Pieces beyond
 // the buffer read as zero.
 int scale_map(CUtensorMap *m, const void *base, int64_t rows, int64_t pieces) {
-    EncodeTiledFn fn = encode_fn();
+    EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return SVDCACHE_ERR_CUDA;
     const cuuint64_t dims[2] = {(cuuint64_t)pieces * (kScalePieceBytes / 4), (cuuint64_t)((rows + kScaleRows - 1) / kScaleRows)};
     const cuuint64_t strides[1] = {(cuuint64_t)pieces * kScalePieceBytes};
@@ -1096,7 +1062,7 @@ int scale_map(CUtensorMap *m, const void *base, int64_t rows, int64_t pieces) {
 
 // C in boxes of 32 rows x 128 bytes; what lies beyond M or N is not written
 int out_map(CUtensorMap *m, const GemmFp8Args &a) {
-    EncodeTiledFn fn = encode_fn();
+    EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return SVDCACHE_ERR_CUDA;
     const int elem = a.out == SVDCACHE_FP8 ? 1 : a.out == SVDCACHE_BF16 ? 2 : 4;
     const CUtensorMapDataType t = a.out == SVDCACHE_FP8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
@@ -1305,7 +1271,7 @@ int gemm_fp8_adapters_launch(const GemmFp8Args &a, const AdapterCall &c, const G
         part.M = std::min(band, a.M - first);
         part.A = (const char *)a.A + first * a.lda;
         part.SA = (const char *)a.SA + first / kScaleRows * fp8_piece_cols(a.K) * kScalePieceBytes;
-        part.C = (char *)a.C + first * a.ldc * (a.out == SVDCACHE_F32 ? 4 : a.out == SVDCACHE_BF16 ? 2 : 1);
+        part.C = (float *)a.C + first * a.ldc;       // fp32 alone has several bands
         AdapterCall call = c;
         call.first = first;
         const AdapterUse use{&call, adapter_layout(part.M, tile_rows, c.pool.rank, c.requests, parts), tile_rows};
